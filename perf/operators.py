@@ -1,0 +1,437 @@
+"""Attention of ordinary tokens beside the proxies, as measurable calls.
+
+A case is a dict of plain values. `op` says which operator a pass calls:
+
+  forward   binding.qk_norm_rope_forward: queries and keys normed per head and
+            turned by their positions, in training
+  backward  binding.qk_norm_rope_backward: its gradients
+  append    binding.PagedCache.append: the same norm and rotation for new tokens,
+            whose keys and values go into the pages of a cache
+  attend    binding.PagedCache.attend: one new token of every sequence over a
+            paged cache, all of it or a window and the first tokens
+
+`own` chooses between the framework's kernels and the operators' plain form
+in elementary torch operations. Head layouts are those of synth.py's workloads
+(16 x 64, 8 x 64, 16 x 128) and generic ones with shared keys and values.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+EPS = 1e-6
+BASE = 10000.0
+
+
+def _heads(op, heads, kv, dim, dtype="bf16", norm=True, rot=None, style="halves", axes=""):
+    return {"op": op, "heads": heads, "kv": kv, "dim": dim, "dtype": dtype, "norm": norm,
+            "rot": dim if rot is None else rot, "style": style, "axes": axes}
+
+
+def _qk(name, op, heads, kv, dim, tokens, **kw):
+    return dict({"name": name} if name else {}, **_heads(op, heads, kv, dim, **kw), tokens=tokens)
+
+
+def _append(name, heads, kv, dim, batch, new, cached, page, ragged=False, lens=0, **kw):
+    return dict({"name": name} if name else {}, **_heads("append", heads, kv, dim, **kw), batch=batch, new=new,
+                cached=cached, page=page, ragged=ragged, lens=lens)
+
+
+def _attend(name, heads, kv, dim, batch, longest, page, window=0, sinks=0, ragged=False, lens=0, dtype="bf16"):
+    return dict({"name": name} if name else {}, **_heads("attend", heads, kv, dim, dtype=dtype), batch=batch,
+                longest=longest, page=page, window=window, sinks=sinks, ragged=ragged, lens=lens)
+
+
+def listed():
+    return [
+        # one new token of one user: the smallest call of all
+        _qk("forward_1_token", "forward", 16, 16, 64, 1),
+        # a training batch of 64K tokens, keys shared by four query heads
+        _qk("forward_64k_gqa", "forward", 16, 4, 128, 65536),
+        # a short clip in single precision: time, height and width as positions
+        _qk("forward_video_fp32", "forward", 8, 8, 64, 5003, dtype="fp32", axes="8,12,12"),
+        # the training step's way back through 64K tokens of the 16 x 64 layer
+        _qk("backward_64k", "backward", 16, 16, 64, 65536),
+        # an odd batch in single precision, half of each head turned, neighbours paired
+        _qk("backward_4099_fp32", "backward", 8, 2, 128, 4099, dtype="fp32", rot=64, style="pairs"),
+        # one serving step: a token of each of 32 sequences
+        _append("append_32_tokens", 16, 16, 64, 32, 1, 480, 64, ragged=True, lens=1),
+        # prompts of many lengths taken in together, behind what is cached
+        _append("append_prompts", 32, 8, 128, 24, 2600, 700, 16, ragged=True, lens=2),
+        # one user early in a conversation
+        _attend("attend_1_short", 8, 8, 64, 1, 200, 16),
+        # continuous batching: sequences of many lengths, a slot or two empty
+        _attend("attend_ragged_gqa", 32, 8, 128, 48, 9000, 16, ragged=True, lens=3),
+        # batch serving against long caches, the repository's decode workload
+        _attend("attend_32_16k", 16, 16, 64, 32, 16384, 64),
+        # one document of a million tokens
+        _attend("attend_1_1M", 32, 8, 128, 1, 1 << 20, 128),
+        # a windowed layer with its first tokens in sight, in single precision
+        _attend("attend_window_fp32", 8, 4, 64, 24, 20000, 32, window=2000, sinks=4, ragged=True, lens=4, dtype="fp32"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    largest = {c["op"]: 0 for c in listed()}
+    for c in listed():
+        largest[c["op"]] = max(largest[c["op"]], _cost(c))
+    while True:
+        op = rng.choice(["forward", "backward", "append", "attend", "attend"])
+        dim = rng.choice([64, 128])
+        kv = rng.choice([1, 2, 3, 4, 8, 16])
+        heads = kv * rng.choice([1, 1, 2, 4, 5, 8, 16])
+        dtype = rng.choice(["bf16", "bf16", "bf16", "fp32"])
+        kw = {"dtype": dtype, "norm": rng.random() < 0.75, "style": rng.choice(["halves", "halves", "pairs"]),
+              "rot": rng.choice([dim, dim, dim // 2, 16])}
+        if rng.random() < 0.3:
+            first = rng.randint(1, kw["rot"] // 2 - 2)
+            second = rng.randint(1, kw["rot"] // 2 - first - 1)
+            kw["axes"] = "%d,%d,%d" % (first, second, kw["rot"] // 2 - first - second)
+        page = 16 * rng.choice([1, 1, 2, 3, 4, 8, 16])
+        lens = rng.randrange(1 << 30)
+        if op in ("forward", "backward"):
+            c = _qk(None, op, heads, kv, dim, _log(rng, 1, 131072), **kw)
+        elif op == "append":
+            kw.pop("axes", None)
+            c = _append(None, heads, kv, dim, _log(rng, 1, 128), rng.choice([1, _log(rng, 2, 16384)]),
+                        _log(rng, 1, 4096), page, rng.random() < 0.7, lens, **kw)
+        else:
+            window = rng.choice([0, 0, _log(rng, 1, 8192)])
+            c = _attend(None, heads, kv, dim, _log(rng, 1, 128), _log(rng, 1, 1 << 20), page, window,
+                        rng.choice([0, 1, 4, 40]) if window else 0, rng.random() < 0.7, lens, dtype)
+        if heads <= 64 and _cost(c) <= largest[op]:
+            return c
+
+
+# ---------------------------------------------------------------- sizes
+
+def _size(case):
+    return 2 if case["dtype"] == "bf16" else 4
+
+
+def _lengths(case):
+    """Cached tokens of every sequence (attend), a few slots empty where ragged."""
+    rng = random.Random(case["lens"])
+    n = [case["longest"]]
+    while len(n) < case["batch"]:
+        n.append(case["longest"] if not case["ragged"] else 0 if rng.random() < 0.04 else rng.randint(1, case["longest"]))
+    return n
+
+
+def _append_lengths(case):
+    """(cached before, new) of every sequence (append)."""
+    rng = random.Random(case["lens"])
+    n = [(case["cached"], case["new"])]
+    while len(n) < case["batch"]:
+        n.append((rng.randint(0, case["cached"]) if case["ragged"] else case["cached"],
+                  rng.randint(0, case["new"]) if case["ragged"] and case["new"] > 1 else case["new"]))
+    return n
+
+
+def _pages(case):
+    """Pages of every sequence."""
+    lens = _lengths(case) if case["op"] == "attend" else [a + b for a, b in _append_lengths(case)]
+    return [-(-n // case["page"]) for n in lens]
+
+
+def _visible(case):
+    w, s = case["window"], case["sinks"]
+    return [n if not w or n <= w else w + min(s, n - w) for n in _lengths(case)]
+
+
+def _cost(case):
+    """What bounds a draw: the bytes of a pass, and of the cache that stands behind it."""
+    held = sum(_pages(case)) * case["page"] * case["kv"] * case["dim"] * _size(case) * 2 if case["op"] in ("append", "attend") else 0
+    return max(work(case)["bytes"], held // 2)
+
+
+def work(case):
+    es, d, hq, hk = _size(case), case["dim"], case["heads"], case["kv"]
+    if case["op"] == "attend":
+        vis = sum(_visible(case))
+        tables = 4 * (sum(_pages(case)) + case["batch"])
+        return {"bytes": 2 * vis * hk * d * es + 2 * case["batch"] * hq * d * es + tables, "flops": 4 * vis * hq * d}
+    gammas = 2 * d * es if case["norm"] else 0
+    if case["op"] == "append":
+        t = sum(n for _, n in _append_lengths(case))
+        small = gammas + 4 * case["rot"] + 4 * (2 * case["batch"] + sum(_pages(case)))
+        return {"bytes": t * (2 * hq + 4 * hk) * d * es + small, "flops": t * (hq + hk) * d * 7}
+    t = case["tokens"]
+    small = gammas + 4 * case["rot"] + 4 * t * _axes(case)
+    if case["op"] == "forward":
+        return {"bytes": 2 * t * (hq + hk) * d * es + small, "flops": t * (hq + hk) * d * 7}
+    return {"bytes": 3 * t * (hq + hk) * d * es + small + (8 * d if case["norm"] else 0), "flops": t * (hq + hk) * d * 15}
+
+
+def _axes(case):
+    return len(_sections(case))
+
+
+def _sections(case):
+    return [int(n) for n in case["axes"].split(",")] if case["axes"] else [case["rot"] // 2]
+
+
+# ---------------------------------------------------------------- inputs
+
+def prepare(case, seed):
+    """Inputs from the seed; sizes and lengths go by the case alone."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    dt = torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+    hq, hk, d = case["heads"], case["kv"], case["dim"]
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device="cuda", dtype=dt)
+
+    def whole(n):
+        return torch.tensor(n, dtype=torch.int32, device="cuda")
+
+    st = {"case": case}
+    if case["op"] != "attend":
+        # angular frequencies of the pairs, from 1 down, anew for every axis
+        st["freqs"] = torch.cat([BASE ** (-torch.arange(n, dtype=torch.float64) / n) for n in _sections(case)]).cuda()
+        st["gamma_q"], st["gamma_k"] = ((1 + 0.1 * normal(d)), (1 + 0.1 * normal(d))) if case["norm"] else (None, None)
+    if case["op"] in ("forward", "backward"):
+        t = case["tokens"]
+        qkv = normal(t, hq + 2 * hk, d)  # as one projection writes them
+        st["q"], st["k"] = qkv[:, :hq], qkv[:, hq:hq + hk]
+        far = torch.randint(0, 1 << 20, (1,), generator=gen, device="cuda", dtype=torch.int32)
+        if case["axes"]:
+            at = torch.arange(t, device="cuda", dtype=torch.int32)
+            st["positions"] = torch.stack([(at // 256) + far % 500, (at // 16) % 16, at % 16][:_axes(case)])
+        else:
+            st["positions"] = (torch.arange(t, device="cuda", dtype=torch.int32) + far)[None]
+        if case["op"] == "backward":
+            st["dq_out"], st["dk_out"] = normal(t, hq, d), normal(t, hk, d)
+    else:
+        n_pages = sum(_pages(case)) + 3
+        st["k_pages"], st["v_pages"] = normal(n_pages, hk, case["page"], d), normal(n_pages, hk, case["page"], d)
+        order = torch.randperm(n_pages, generator=gen, device="cuda").to(torch.int32)
+        table = torch.full((case["batch"], max(_pages(case))), -1, dtype=torch.int32)
+        starts = [0]
+        for n in _pages(case):
+            starts.append(starts[-1] + n)
+        cols = torch.arange(table.shape[1])[None] + torch.tensor(starts[:-1])[:, None]
+        used = torch.arange(table.shape[1])[None] < torch.tensor(_pages(case))[:, None]
+        st["table"] = torch.where(used, order.cpu()[cols.clamp(max=n_pages - 1)], table).cuda()
+        if case["op"] == "attend":
+            st["q"] = normal(case["batch"], hq, d) * 2
+            st["kv_len"] = whole(_lengths(case))
+        else:
+            lens = _append_lengths(case)
+            st["tokens"] = sum(n for _, n in lens)
+            rows = st["tokens"] if case["new"] == 1 or not case["ragged"] else -(-st["tokens"] // 64) * 64  # a padded batch
+            qkv = normal(rows, hq + 2 * hk, d)
+            st["q"], st["k"], st["v"] = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]
+            st["q_out"] = torch.zeros(rows, hq, d, device="cuda", dtype=dt)
+            st["kv_len"] = whole([a + b for a, b in lens])
+            cu = [0]
+            for _, n in lens:
+                cu.append(cu[-1] + n)
+            st["cu"] = None if case["new"] == 1 else whole(cu)
+    if own:
+        from paper_2608_23463_amd import binding as B
+        st["cfg"] = B.heads_config(hq, hk, d, dtype=case["dtype"], norm=case["norm"], eps=EPS, rot_dim=case["rot"],
+                                   style=B.PF_ROPE_PAIRS if case["style"] == "pairs" else B.PF_ROPE_HALVES,
+                                   axis_pairs=_sections(case) if case["axes"] else ())
+        st["weights"] = {k: st.get(k) for k in ("gamma_q", "gamma_k", "freqs")}
+        if "table" in st:
+            st["cache"] = B.PagedCache(st["cfg"], st["weights"], st["k_pages"], st["v_pages"], st["table"], st["kv_len"])
+    return st
+
+
+# ---------------------------------------------------------------- a pass
+
+def run(st):
+    case = st["case"]
+    if own:
+        return _own(case, st)
+    if case["op"] == "forward":
+        turn = _turn(case, st["positions"], st["freqs"])
+        return [_norm_rope(case, st[x], st["gamma_" + x], turn).to(st[x].dtype) for x in ("q", "k")]
+    if case["op"] == "backward":
+        turn = _turn(case, st["positions"], st["freqs"])
+        dq, dgq = _norm_rope_backward(case, st["q"], st["gamma_q"], turn, st["dq_out"])
+        dk, dgk = _norm_rope_backward(case, st["k"], st["gamma_k"], turn, st["dk_out"])
+        return [dq, dk, dgq, dgk]
+    if case["op"] == "append":
+        return _plain_append(case, st)
+    return _plain_attend(case, st)
+
+
+def _own(case, st):
+    from paper_2608_23463_amd import binding as B
+    if case["op"] == "forward":
+        return B.qk_norm_rope_forward(st["cfg"], st["weights"], st["q"], st["k"], st["positions"])
+    if case["op"] == "backward":
+        return B.qk_norm_rope_backward(st["cfg"], st["weights"], st["q"], st["k"], st["positions"], st["dq_out"],
+                                       st["dk_out"])
+    if case["op"] == "append":
+        st["cache"].append(st["k"], st["v"], q=st["q"], cu_tokens=st["cu"], q_out=st["q_out"])
+        return [st["q_out"], st["k_pages"], st["v_pages"]]
+    return st["cache"].attend(st["q"], case["longest"], window=case["window"], sinks=case["sinks"])
+
+
+def _turn(case, positions, freqs):
+    """cos and sin [T, 1, rot / 2] of positions [axes, T]: angles in 64 bits."""
+    axis = torch.repeat_interleave(torch.arange(_axes(case), device=freqs.device),
+                                   torch.tensor(_sections(case), device=freqs.device), output_size=freqs.numel())
+    angle = positions[axis].double().t() * freqs
+    return angle.cos().float()[:, None], angle.sin().float()[:, None]
+
+
+def _halves(case, z):
+    r = case["rot"]
+    return (z[..., 0:r:2], z[..., 1:r:2]) if case["style"] == "pairs" else (z[..., :r // 2], z[..., r // 2:r])
+
+
+def _rotated(case, z, cos, sin):
+    out = z.clone()
+    a, b = _halves(case, z)
+    oa, ob = _halves(case, out)
+    oa.copy_(a * cos - b * sin)
+    ob.copy_(a * sin + b * cos)
+    return out
+
+
+def _norm_rope(case, x, gamma, turn):
+    z = x.float()
+    if case["norm"]:
+        z = z * torch.rsqrt((z * z).mean(-1, keepdim=True) + EPS) * gamma.float()
+    return _rotated(case, z, *turn)
+
+
+def _norm_rope_backward(case, x, gamma, turn, dy):
+    dz = _rotated(case, dy.float(), turn[0], -turn[1])
+    if not case["norm"]:
+        return dz.to(x.dtype), None
+    xf = x.float()
+    rstd = torch.rsqrt((xf * xf).mean(-1, keepdim=True) + EPS)
+    xn = xf * rstd
+    g = dz * gamma.float()
+    dx = rstd * (g - xn * (g * xn).mean(-1, keepdim=True))
+    return dx.to(x.dtype), (dz * xn).sum((0, 1), dtype=torch.float64).float()
+
+
+def _plain_append(case, st):
+    n, page = st["tokens"], case["page"]
+    at = torch.arange(n, device="cuda")
+    if st["cu"] is None:
+        seq, pos = at, st["kv_len"].long() - 1
+    else:
+        cu = st["cu"].long()
+        seq = torch.searchsorted(cu[1:], at, right=True)
+        pos = st["kv_len"].long()[seq] - cu[seq + 1] + at
+    turn = _turn(case, pos[None].expand(_axes(case), -1), st["freqs"])
+    ids, slot = st["table"].long()[seq, pos // page], pos % page
+    st["k_pages"][ids, :, slot] = _norm_rope(case, st["k"][:n], st["gamma_k"], turn).to(st["k"].dtype)
+    st["v_pages"][ids, :, slot] = st["v"][:n]
+    st["q_out"][:n] = _norm_rope(case, st["q"][:n], st["gamma_q"], turn).to(st["q"].dtype)
+    return [st["q_out"], st["k_pages"], st["v_pages"]]
+
+
+def _plain_attend(case, st):
+    b, hq, hk, d, page = case["batch"], case["heads"], case["kv"], case["dim"], case["page"]
+    lens = st["kv_len"].long()[:, None]
+    w, s = case["window"], case["sinks"]
+    if w:  # the first tokens, then the window
+        sink = torch.arange(min(s, case["longest"]), device="cuda")[None].expand(b, -1)
+        first = (lens - w).clamp(min=0)
+        last = first + torch.arange(min(w, case["longest"]), device="cuda")[None]
+        pos, seen = torch.cat([sink, last], 1), torch.cat([sink < first, last < lens], 1)
+    else:
+        pos = torch.arange(case["longest"], device="cuda")[None].expand(b, -1)
+        seen = pos < lens
+    safe = torch.where(seen, pos, 0)
+    ids = torch.gather(st["table"].long(), 1, safe // page).clamp(min=0)
+    k = st["k_pages"][ids, :, safe % page].float().permute(0, 2, 3, 1).contiguous()  # [B, Hk, D, L]
+    q = st["q"].float().reshape(b, hk, hq // hk, d)
+    scores = torch.matmul(q, k) / math.sqrt(d)
+    scores = scores.masked_fill(~seen[:, None, None], -math.inf)
+    top = scores.amax(-1, keepdim=True).clamp(min=-1e30)
+    p = torch.exp(scores - top)
+    p = p / p.sum(-1, keepdim=True).clamp(min=1e-30)  # an empty slot stays zero
+    v = st["v_pages"][ids, :, safe % page].float().permute(0, 2, 1, 3).contiguous()
+    return torch.matmul(p, v).reshape(b, hq, d).to(st["q"].dtype)
+
+
+# ---------------------------------------------------------------- 64 bits
+
+def exact(case, seed):
+    """From the definitions in 64 bits: rotations as complex factors, gradients
+    by automatic differentiation, attention one sequence and head at a time."""
+    st = prepare(case, seed)
+    if case["op"] == "forward":
+        phase = _phase(case, st["positions"], st["freqs"])
+        return [_defined(case, st[x].double(), _wide(st["gamma_" + x]), phase) for x in ("q", "k")]
+    if case["op"] == "backward":
+        phase = _phase(case, st["positions"], st["freqs"])
+        grads, gains = [], []
+        for x in ("q", "k"):
+            leaf, gamma = st[x].double().requires_grad_(), _wide(st["gamma_" + x])
+            leaves = [leaf] if gamma is None else [leaf, gamma.requires_grad_()]
+            got = torch.autograd.grad(_defined(case, leaf, gamma, phase), leaves, st["d%s_out" % x].double())
+            grads.append(got[0])
+            gains.append(got[1] if gamma is not None else None)
+        return grads + gains
+    if case["op"] == "append":
+        q_out, kp, vp = st["q_out"].double(), st["k_pages"].double(), st["v_pages"].double()
+        row = 0
+        for i, (cached, new) in enumerate(_append_lengths(case)):
+            if new:
+                pos = torch.arange(cached, cached + new, device="cuda")
+                phase = _phase(case, torch.stack([pos] * _axes(case)), st["freqs"])
+                rows = slice(row, row + new)
+                q_out[rows] = _defined(case, st["q"][rows].double(), _wide(st["gamma_q"]), phase)
+                ids = st["table"][i].long()[pos // case["page"]]
+                kp[ids, :, pos % case["page"]] = _defined(case, st["k"][rows].double(), _wide(st["gamma_k"]), phase)
+                vp[ids, :, pos % case["page"]] = st["v"][rows].double()
+                row += new
+        return [q_out, kp, vp]
+    out = torch.zeros(st["q"].shape, dtype=torch.float64, device="cuda")
+    share = case["heads"] // case["kv"]
+    for i, n in enumerate(_lengths(case)):
+        if n == 0:
+            continue
+        pages = st["table"][i, :-(-n // case["page"])].long()
+        at = torch.arange(n, device="cuda")
+        out_of_sight = (at < n - case["window"]) & (at >= case["sinks"]) if case["window"] else at < 0
+        for h in range(case["kv"]):
+            k = st["k_pages"][pages, h].reshape(-1, case["dim"])[:n].double()
+            v = st["v_pages"][pages, h].reshape(-1, case["dim"])[:n].double()
+            q = st["q"][i, h * share:(h + 1) * share].double()
+            logits = (q @ k.t()) * case["dim"] ** -0.5
+            logits[:, out_of_sight] = -math.inf
+            out[i, h * share:(h + 1) * share] = torch.softmax(logits, -1) @ v
+    return out
+
+
+def _wide(t):
+    return None if t is None else t.double()
+
+
+def _phase(case, positions, freqs):
+    """exp(i * angle) of every token and pair, one axis after another."""
+    parts, at = [], 0
+    for axis, n in enumerate(_sections(case)):
+        parts.append(positions[axis].double()[:, None] * freqs[at:at + n][None])
+        at += n
+    angle = torch.cat(parts, 1)
+    return torch.polar(torch.ones_like(angle), angle)[:, None]
+
+
+def _defined(case, x, gamma, phase):
+    if case["norm"]:
+        x = x / torch.sqrt(x.square().mean(-1, keepdim=True) + EPS) * gamma
+    r = case["rot"]
+    if case["style"] == "pairs":
+        turned = torch.view_as_real(torch.view_as_complex(x[..., :r].unflatten(-1, (-1, 2)).contiguous()) * phase).flatten(-2)
+    else:
+        c = torch.complex(x[..., :r // 2], x[..., r // 2:r]) * phase
+        turned = torch.cat([c.real, c.imag], -1)
+    return torch.cat([turned, x[..., r:]], -1)
