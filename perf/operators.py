@@ -7,8 +7,9 @@ A case is a dict of plain values. `op` says which operator a pass calls:
   backward  binding.qk_norm_rope_backward: its gradients
   append    binding.PagedCache.append: the same norm and rotation for new tokens,
             whose keys and values go into the pages of a cache
-  attend    binding.PagedCache.attend: one new token of every sequence over a
-            paged cache, all of it or a window and the first tokens
+  attend    binding.PagedCache.attend: the new tokens of every sequence, one or
+            a prompt, over a paged cache: all of it up to each token's own row,
+            or a window and the first rows
 
 `own` chooses between the framework's kernels and the operators' plain form
 in elementary torch operations. Head layouts are those of synth.py's workloads
@@ -34,42 +35,39 @@ def _qk(name, op, heads, kv, dim, tokens, **kw):
     return dict({"name": name} if name else {}, **_heads(op, heads, kv, dim, **kw), tokens=tokens)
 
 
-def _append(name, heads, kv, dim, batch, new, cached, page, ragged=False, lens=0, **kw):
-    return dict({"name": name} if name else {}, **_heads("append", heads, kv, dim, **kw), batch=batch, new=new,
-                cached=cached, page=page, ragged=ragged, lens=lens)
-
-
-def _attend(name, heads, kv, dim, batch, longest, page, window=0, sinks=0, ragged=False, lens=0, dtype="bf16"):
-    return dict({"name": name} if name else {}, **_heads("attend", heads, kv, dim, dtype=dtype), batch=batch,
-                longest=longest, page=page, window=window, sinks=sinks, ragged=ragged, lens=lens)
+def _paged(name, op, heads, kv, dim, batch, new, cached, page, window=0, sinks=0, ragged=False, lens=0, **kw):
+    return dict({"name": name} if name else {}, **_heads(op, heads, kv, dim, **kw), batch=batch, new=new,
+                cached=cached, page=page, window=window, sinks=sinks, ragged=ragged, lens=lens)
 
 
 def listed():
     return [
-        # one new token of one user: the smallest call of all
-        _qk("forward_1_token", "forward", 16, 16, 64, 1),
         # a training batch of 64K tokens, keys shared by four query heads
         _qk("forward_64k_gqa", "forward", 16, 4, 128, 65536),
-        # a short clip in single precision: time, height and width as positions
-        _qk("forward_video_fp32", "forward", 8, 8, 64, 5003, dtype="fp32", axes="8,12,12"),
         # the training step's way back through 64K tokens of the 16 x 64 layer
         _qk("backward_64k", "backward", 16, 16, 64, 65536),
-        # an odd batch in single precision, half of each head turned, neighbours paired
-        _qk("backward_4099_fp32", "backward", 8, 2, 128, 4099, dtype="fp32", rot=64, style="pairs"),
+        # a short clip in single precision: time, height and width as positions
+        # of half of each head, neighbours paired
+        _qk("backward_video_fp32", "backward", 8, 2, 128, 5003, dtype="fp32", rot=64, style="pairs", axes="8,12,12"),
         # one serving step: a token of each of 32 sequences
-        _append("append_32_tokens", 16, 16, 64, 32, 1, 480, 64, ragged=True, lens=1),
+        _paged("append_32_tokens", "append", 16, 16, 64, 32, 1, 480, 64, ragged=True, lens=1),
         # prompts of many lengths taken in together, behind what is cached
-        _append("append_prompts", 32, 8, 128, 24, 2600, 700, 16, ragged=True, lens=2),
-        # one user early in a conversation
-        _attend("attend_1_short", 8, 8, 64, 1, 200, 16),
+        _paged("append_prompts", "append", 32, 8, 128, 24, 2600, 700, 16, ragged=True, lens=2),
+        # one user early in a conversation: the smallest call
+        _paged("attend_1_short", "attend", 8, 8, 64, 1, 1, 199, 16),
         # continuous batching: sequences of many lengths, a slot or two empty
-        _attend("attend_ragged_gqa", 32, 8, 128, 48, 9000, 16, ragged=True, lens=3),
+        _paged("attend_ragged_gqa", "attend", 32, 8, 128, 48, 1, 9000, 16, ragged=True, lens=3),
         # batch serving against long caches, the repository's decode workload
-        _attend("attend_32_16k", 16, 16, 64, 32, 16384, 64),
+        _paged("attend_32_16k", "attend", 16, 16, 64, 32, 1, 16383, 64),
         # one document of a million tokens
-        _attend("attend_1_1M", 32, 8, 128, 1, 1 << 20, 128),
+        _paged("attend_1_1M", "attend", 32, 8, 128, 1, 1, (1 << 20) - 1, 128),
         # a windowed layer with its first tokens in sight, in single precision
-        _attend("attend_window_fp32", 8, 4, 64, 24, 20000, 32, window=2000, sinks=4, ragged=True, lens=4, dtype="fp32"),
+        _paged("attend_window_fp32", "attend", 8, 4, 64, 24, 1, 20000, 32, window=2000, sinks=4, ragged=True, lens=4,
+               dtype="fp32"),
+        # prompts of a windowed layer, some behind a cached beginning
+        _paged("attend_prompts_window", "attend", 16, 16, 64, 6, 2048, 1500, 64, window=700, sinks=4, ragged=True, lens=5),
+        # one long prompt from the start
+        _paged("attend_prompt_8k", "attend", 32, 8, 128, 1, 8192, 0, 16),
     ]
 
 
@@ -78,11 +76,8 @@ def _log(rng, lo, hi):
 
 
 def draw(rng):
-    largest = {c["op"]: 0 for c in listed()}
-    for c in listed():
-        largest[c["op"]] = max(largest[c["op"]], _cost(c))
     while True:
-        op = rng.choice(["forward", "backward", "append", "attend", "attend"])
+        op = rng.choice(["forward", "backward", "append", "attend", "attend", "attend"])
         dim = rng.choice([64, 128])
         kv = rng.choice([1, 2, 3, 4, 8, 16])
         heads = kv * rng.choice([1, 1, 2, 4, 5, 8, 16])
@@ -94,19 +89,30 @@ def draw(rng):
             second = rng.randint(1, kw["rot"] // 2 - first - 1)
             kw["axes"] = "%d,%d,%d" % (first, second, kw["rot"] // 2 - first - second)
         page = 16 * rng.choice([1, 1, 2, 3, 4, 8, 16])
-        lens = rng.randrange(1 << 30)
+        lens, ragged = rng.randrange(1 << 30), rng.random() < 0.7
         if op in ("forward", "backward"):
             c = _qk(None, op, heads, kv, dim, _log(rng, 1, 131072), **kw)
         elif op == "append":
             kw.pop("axes", None)
-            c = _append(None, heads, kv, dim, _log(rng, 1, 128), rng.choice([1, _log(rng, 2, 16384)]),
-                        _log(rng, 1, 4096), page, rng.random() < 0.7, lens, **kw)
+            c = _paged(None, op, heads, kv, dim, _log(rng, 1, 128), rng.choice([1, _log(rng, 2, 16384)]),
+                       _log(rng, 1, 4096), page, 0, 0, ragged, lens, **kw)
         else:
             window = rng.choice([0, 0, _log(rng, 1, 8192)])
-            c = _attend(None, heads, kv, dim, _log(rng, 1, 128), _log(rng, 1, 1 << 20), page, window,
-                        rng.choice([0, 1, 4, 40]) if window else 0, rng.random() < 0.7, lens, dtype)
-        if heads <= 64 and _cost(c) <= largest[op]:
+            new = rng.choice([1, 1, _log(rng, 2, 8192)])
+            c = _paged(None, op, heads, kv, dim, _log(rng, 1, 128), new,
+                       _log(rng, 1, 1 << 20 if new == 1 else 8192) - 1, page, window,
+                       rng.choice([0, 1, 4, 40]) if window else 0, ragged, lens, dtype=dtype)
+        if heads <= 64 and _fits(c):
             return c
+
+
+def _fits(case):
+    """Whether a case costs no more than the largest listed one of its operator,
+    in bytes, in operations and in what the plain form spreads out."""
+    for f in (lambda c: work(c)["bytes"], lambda c: work(c)["flops"] * (1 if c["dtype"] == "bf16" else 8), _held, _spread):
+        if f(case) > max(f(c) for c in listed() if c["op"] == case["op"]):
+            return False
+    return True
 
 
 # ---------------------------------------------------------------- sizes
@@ -116,50 +122,67 @@ def _size(case):
 
 
 def _lengths(case):
-    """Cached tokens of every sequence (attend), a few slots empty where ragged."""
+    """(cached rows with the new ones, new tokens) of every sequence. In a step
+    of one token each, a few slots of a ragged attention are empty."""
     rng = random.Random(case["lens"])
-    n = [case["longest"]]
+    single = case["new"] == 1
+    n = [(case["cached"] + case["new"], case["new"])]
     while len(n) < case["batch"]:
-        n.append(case["longest"] if not case["ragged"] else 0 if rng.random() < 0.04 else rng.randint(1, case["longest"]))
-    return n
-
-
-def _append_lengths(case):
-    """(cached before, new) of every sequence (append)."""
-    rng = random.Random(case["lens"])
-    n = [(case["cached"], case["new"])]
-    while len(n) < case["batch"]:
-        n.append((rng.randint(0, case["cached"]) if case["ragged"] else case["cached"],
-                  rng.randint(0, case["new"]) if case["ragged"] and case["new"] > 1 else case["new"]))
+        if not case["ragged"]:
+            n.append(n[0])
+        elif single and case["op"] == "attend" and rng.random() < 0.04:
+            n.append((0, 1))
+        else:
+            new = 1 if single else rng.randint(0, case["new"])
+            n.append((rng.randint(0, case["cached"]) + new, new))
     return n
 
 
 def _pages(case):
     """Pages of every sequence."""
-    lens = _lengths(case) if case["op"] == "attend" else [a + b for a, b in _append_lengths(case)]
-    return [-(-n // case["page"]) for n in lens]
+    return [-(-n // case["page"]) for n, _ in _lengths(case)]
+
+
+def _tokens(case):
+    return sum(new for _, new in _lengths(case))
 
 
 def _visible(case):
+    """(rows that any token sees, rows seen summed over the tokens) of every sequence."""
     w, s = case["window"], case["sinks"]
-    return [n if not w or n <= w else w + min(s, n - w) for n in _lengths(case)]
+    out = []
+    for n, new in _lengths(case):
+        new = min(new, n)
+        row = torch.arange(n - new, n)
+        seen = row + 1 if not w else (row + 1).clamp(max=w) + (row + 1 - w).clamp(min=0, max=s)
+        lo = max(0, n - new + 1 - w) if w else 0
+        out.append((n - lo + min(s, lo) if new else 0, int(seen.sum())))
+    return out
 
 
-def _cost(case):
-    """What bounds a draw: the bytes of a pass, and of the cache that stands behind it."""
-    held = sum(_pages(case)) * case["page"] * case["kv"] * case["dim"] * _size(case) * 2 if case["op"] in ("append", "attend") else 0
-    return max(work(case)["bytes"], held // 2)
+def _held(case):
+    """Bytes of the cache behind a pass."""
+    return 0 if "page" not in case else 2 * sum(_pages(case)) * case["page"] * case["kv"] * case["dim"] * _size(case)
+
+
+def _spread(case):
+    """Scores that an attention in its plain form spreads out."""
+    if case["op"] != "attend":
+        return 0
+    rows = min(case["cached"] + case["new"], case["window"] + case["sinks"]) if case["window"] and case["new"] == 1 else case["cached"] + case["new"]
+    return case["batch"] * case["new"] * rows * max(case["heads"], case["kv"] * case["dim"] // case["new"])
 
 
 def work(case):
     es, d, hq, hk = _size(case), case["dim"], case["heads"], case["kv"]
     if case["op"] == "attend":
-        vis = sum(_visible(case))
-        tables = 4 * (sum(_pages(case)) + case["batch"])
-        return {"bytes": 2 * vis * hk * d * es + 2 * case["batch"] * hq * d * es + tables, "flops": 4 * vis * hq * d}
+        seen = _visible(case)
+        small = 4 * (sum(_pages(case)) + 2 * case["batch"])
+        return {"bytes": 2 * sum(n for n, _ in seen) * hk * d * es + 2 * _tokens(case) * hq * d * es + small,
+                "flops": 4 * sum(n for _, n in seen) * hq * d}
     gammas = 2 * d * es if case["norm"] else 0
     if case["op"] == "append":
-        t = sum(n for _, n in _append_lengths(case))
+        t = _tokens(case)
         small = gammas + 4 * case["rot"] + 4 * (2 * case["batch"] + sum(_pages(case)))
         return {"bytes": t * (2 * hq + 4 * hk) * d * es + small, "flops": t * (hq + hk) * d * 7}
     t = case["tokens"]
@@ -219,21 +242,21 @@ def prepare(case, seed):
         cols = torch.arange(table.shape[1])[None] + torch.tensor(starts[:-1])[:, None]
         used = torch.arange(table.shape[1])[None] < torch.tensor(_pages(case))[:, None]
         st["table"] = torch.where(used, order.cpu()[cols.clamp(max=n_pages - 1)], table).cuda()
+        lens, single = _lengths(case), case["new"] == 1
+        st["kv_len"] = whole([n for n, _ in lens])
+        st["tokens"] = _tokens(case)
+        rows = st["tokens"] if single or not case["ragged"] else -(-st["tokens"] // 64) * 64  # a padded batch
+        cu = [0]
+        for _, new in lens:
+            cu.append(cu[-1] + new)
+        st["cu"] = None if single else whole(cu)
         if case["op"] == "attend":
-            st["q"] = normal(case["batch"], hq, d) * 2
-            st["kv_len"] = whole(_lengths(case))
+            st["q"] = normal(rows, hq, d) * 2
+            st["out"] = torch.zeros(rows, hq, d, device="cuda", dtype=dt)
         else:
-            lens = _append_lengths(case)
-            st["tokens"] = sum(n for _, n in lens)
-            rows = st["tokens"] if case["new"] == 1 or not case["ragged"] else -(-st["tokens"] // 64) * 64  # a padded batch
             qkv = normal(rows, hq + 2 * hk, d)
             st["q"], st["k"], st["v"] = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]
             st["q_out"] = torch.zeros(rows, hq, d, device="cuda", dtype=dt)
-            st["kv_len"] = whole([a + b for a, b in lens])
-            cu = [0]
-            for _, n in lens:
-                cu.append(cu[-1] + n)
-            st["cu"] = None if case["new"] == 1 else whole(cu)
     if own:
         from paper_2608_23463_amd import binding as B
         st["cfg"] = B.heads_config(hq, hk, d, dtype=case["dtype"], norm=case["norm"], eps=EPS, rot_dim=case["rot"],
@@ -274,7 +297,8 @@ def _own(case, st):
     if case["op"] == "append":
         st["cache"].append(st["k"], st["v"], q=st["q"], cu_tokens=st["cu"], q_out=st["q_out"])
         return [st["q_out"], st["k_pages"], st["v_pages"]]
-    return st["cache"].attend(st["q"], case["longest"], window=case["window"], sinks=case["sinks"])
+    return st["cache"].attend(st["q"], case["cached"] + case["new"], cu_tokens=st["cu"], max_new=case["new"],
+                              window=case["window"], sinks=case["sinks"], out=st["out"])
 
 
 def _turn(case, positions, freqs):
@@ -337,34 +361,50 @@ def _plain_append(case, st):
 
 def _plain_attend(case, st):
     b, hq, hk, d, page = case["batch"], case["heads"], case["kv"], case["dim"], case["page"]
+    new, longest = case["new"], case["cached"] + case["new"]
     lens = st["kv_len"].long()[:, None]
     w, s = case["window"], case["sinks"]
-    if w:  # the first tokens, then the window
-        sink = torch.arange(min(s, case["longest"]), device="cuda")[None].expand(b, -1)
+    if w and new == 1:  # the first rows, then the window
         first = (lens - w).clamp(min=0)
-        last = first + torch.arange(min(w, case["longest"]), device="cuda")[None]
-        pos, seen = torch.cat([sink, last], 1), torch.cat([sink < first, last < lens], 1)
+        sink = torch.arange(min(s, longest), device="cuda")[None].expand(b, -1)
+        last = first + torch.arange(min(w, longest), device="cuda")[None]
+        pos, real = torch.cat([sink, last], 1), torch.cat([sink < first, last < lens], 1)
     else:
-        pos = torch.arange(case["longest"], device="cuda")[None].expand(b, -1)
-        seen = pos < lens
-    safe = torch.where(seen, pos, 0)
+        pos = torch.arange(longest, device="cuda")[None].expand(b, -1)
+        real = pos < lens
+    safe = torch.where(real, pos, 0)
     ids = torch.gather(st["table"].long(), 1, safe // page).clamp(min=0)
     k = st["k_pages"][ids, :, safe % page].float().permute(0, 2, 3, 1).contiguous()  # [B, Hk, D, L]
-    q = st["q"].float().reshape(b, hk, hq // hk, d)
-    scores = torch.matmul(q, k) / math.sqrt(d)
-    scores = scores.masked_fill(~seen[:, None, None], -math.inf)
-    top = scores.amax(-1, keepdim=True).clamp(min=-1e30)
-    p = torch.exp(scores - top)
-    p = p / p.sum(-1, keepdim=True).clamp(min=1e-30)  # an empty slot stays zero
     v = st["v_pages"][ids, :, safe % page].float().permute(0, 2, 1, 3).contiguous()
-    return torch.matmul(p, v).reshape(b, hq, d).to(st["q"].dtype)
+    # the i-th token of every sequence, padded to the most new tokens
+    cu = torch.arange(b + 1, device="cuda") if st["cu"] is None else st["cu"].long()
+    mine = cu[:-1, None] + torch.arange(new, device="cuda")[None]
+    is_token = mine < cu[1:, None]
+    row = lens - (cu[1:] - cu[:-1])[:, None] + torch.arange(new, device="cuda")[None]  # [B, new]
+    seen = real[:, None] & (pos[:, None] <= row[..., None])
+    if w:
+        seen = seen & ((pos[:, None] > row[..., None] - w) | (pos[:, None] < s))
+    q = st["q"][torch.where(is_token, mine, 0)].float()  # [B, new, Hq, D]
+    q = q.reshape(b, new, hk, hq // hk, d).permute(0, 2, 3, 1, 4).reshape(b, hk, -1, d)
+    scores = (torch.matmul(q, k) / math.sqrt(d)).view(b, hk, hq // hk, new, -1)
+    scores.masked_fill_(~seen[:, None, None], -math.inf)
+    p = scores.sub_(scores.amax(-1, keepdim=True).clamp(min=-1e30)).exp_()
+    p /= p.sum(-1, keepdim=True).clamp(min=1e-30)  # an empty slot stays zero
+    o = torch.matmul(p.view(b, hk, -1, p.shape[-1]), v).view(b, hq, new, d).transpose(1, 2).to(st["q"].dtype)
+    if st["cu"] is None:
+        st["out"].copy_(o[:, 0])
+    else:
+        at = torch.arange(st["tokens"], device="cuda")
+        seq = torch.searchsorted(cu[1:], at, right=True)
+        st["out"][:st["tokens"]] = o[seq, at - cu[seq]]
+    return st["out"]
 
 
 # ---------------------------------------------------------------- 64 bits
 
 def exact(case, seed):
     """From the definitions in 64 bits: rotations as complex factors, gradients
-    by automatic differentiation, attention one sequence and head at a time."""
+    by automatic differentiation, attention head by head."""
     st = prepare(case, seed)
     if case["op"] == "forward":
         phase = _phase(case, st["positions"], st["freqs"])
@@ -382,9 +422,9 @@ def exact(case, seed):
     if case["op"] == "append":
         q_out, kp, vp = st["q_out"].double(), st["k_pages"].double(), st["v_pages"].double()
         row = 0
-        for i, (cached, new) in enumerate(_append_lengths(case)):
+        for i, (n, new) in enumerate(_lengths(case)):
             if new:
-                pos = torch.arange(cached, cached + new, device="cuda")
+                pos = torch.arange(n - new, n, device="cuda")
                 phase = _phase(case, torch.stack([pos] * _axes(case)), st["freqs"])
                 rows = slice(row, row + new)
                 q_out[rows] = _defined(case, st["q"][rows].double(), _wide(st["gamma_q"]), phase)
@@ -393,21 +433,24 @@ def exact(case, seed):
                 vp[ids, :, pos % case["page"]] = st["v"][rows].double()
                 row += new
         return [q_out, kp, vp]
-    out = torch.zeros(st["q"].shape, dtype=torch.float64, device="cuda")
+    out = st["out"].double()
     share = case["heads"] // case["kv"]
-    for i, n in enumerate(_lengths(case)):
-        if n == 0:
+    first = 0
+    for i, (n, new) in enumerate(_lengths(case)):
+        rows = slice(first, first + new)
+        first += new
+        if n == 0 or new == 0:
             continue
         pages = st["table"][i, :-(-n // case["page"])].long()
-        at = torch.arange(n, device="cuda")
-        out_of_sight = (at < n - case["window"]) & (at >= case["sinks"]) if case["window"] else at < 0
-        for h in range(case["kv"]):
-            k = st["k_pages"][pages, h].reshape(-1, case["dim"])[:n].double()
-            v = st["v_pages"][pages, h].reshape(-1, case["dim"])[:n].double()
-            q = st["q"][i, h * share:(h + 1) * share].double()
-            logits = (q @ k.t()) * case["dim"] ** -0.5
-            logits[:, out_of_sight] = -math.inf
-            out[i, h * share:(h + 1) * share] = torch.softmax(logits, -1) @ v
+        at, own_row = torch.arange(n, device="cuda"), torch.arange(n - new, n, device="cuda")[:, None]
+        hidden = at > own_row
+        if case["window"]:
+            hidden |= (at <= own_row - case["window"]) & (at >= case["sinks"])
+        for h in range(case["heads"]):
+            k = st["k_pages"][pages, h // share].reshape(-1, case["dim"])[:n].double()
+            v = st["v_pages"][pages, h // share].reshape(-1, case["dim"])[:n].double()
+            logits = (st["q"][rows, h].double() @ k.t()) * case["dim"] ** -0.5
+            out[rows, h] = torch.softmax(logits.masked_fill_(hidden, -math.inf), -1) @ v
     return out
 
 
