@@ -332,6 +332,154 @@ int proxy_decode_prefill(const pf_decode_config* cfg, const pf_decode_weights* w
                          pf_decode_state* st, const void* x, int64_t n_tokens, void* y,
                          void* workspace, size_t ws_bytes, void* stream);
 
+/* ---- Attention of ordinary tokens beside the proxies ----
+ *
+ * The fine tokens' own attention, where it reaches past the current block
+ * (Sec. 5.1 allows rotary positions): queries and keys normed per head and
+ * turned by their positions, a cache in pages, and the attention of new tokens
+ * over it.
+ *
+ * Heads of one call. n_heads query heads share n_kv_heads key/value heads,
+ * n_heads / n_kv_heads of them each, in order (query head h reads key/value
+ * head h / (n_heads / n_kv_heads)); n_heads at most 4096.
+ *  head_dim  64 or 128; dtype pf_dtype of all rows and gains.
+ *  norm      PF_NORM_RMS: z = x / sqrt(mean(x^2) + eps) * gamma over the
+ *            head_dim elements of a row; PF_NORM_NONE: z = x.
+ *  rot_dim   elements that are turned, the first of every row: a multiple of
+ *            16 up to head_dim; 0 turns none.
+ *  rope_style  which elements form pair p: PF_ROPE_HALVES p and
+ *            rot_dim / 2 + p; PF_ROPE_PAIRS 2p and 2p + 1.
+ *  n_axes, axis_pairs  positions have n_axes (1..3) coordinates (a sequence
+ *            has one; an image or a video two or three). The first
+ *            axis_pairs[0] pairs turn by the first coordinate, the next
+ *            axis_pairs[1] by the second, ...; they add up to rot_dim / 2.
+ * Pair p = (a, b) turns by t = coordinate * freqs[p]:
+ *   y_a = z_a cos t - z_b sin t, y_b = z_a sin t + z_b cos t.
+ * The angle is formed in 64 bits, so positions up to 2^31 keep it to 1e-6.
+ * Sums and statistics are fp32; a row is rounded once, when it is stored. */
+#define PF_MAX_AXES 3
+enum pf_head_norm { PF_NORM_NONE = 0, PF_NORM_RMS = 1 };
+enum pf_rope_style { PF_ROPE_HALVES = 0, PF_ROPE_PAIRS = 1 };
+typedef struct {
+  int32_t n_heads, n_kv_heads, head_dim, dtype;
+  int32_t norm; /* pf_head_norm */
+  float eps;
+  int32_t rot_dim, rope_style;
+  int32_t n_axes;
+  int32_t axis_pairs[PF_MAX_AXES];
+} pf_heads_config;
+
+/* gamma_q, gamma_k [head_dim] (NULL: ones), read with PF_NORM_RMS; freqs
+ * [rot_dim / 2] fp64, radians per unit of position (NULL if rot_dim is 0). */
+typedef struct {
+  const void* gamma_q;
+  const void* gamma_k;
+  const double* freqs;
+} pf_heads_weights;
+
+/* Rows [token, head, head_dim] of a caller's tensor: a row is contiguous, and
+ * tokens and heads lie token_stride and head_stride elements apart (both not
+ * negative; rows 16-byte aligned, so multiples of 8 in bf16 and 4 in fp32): a
+ * slice of a fused projection, or heads-first storage. Rows that a call
+ * writes must not share elements with each other. They may be the very rows
+ * they are computed from (same p and strides); other overlaps are refused. */
+typedef struct {
+  void* p;
+  int64_t token_stride, head_stride;
+} pf_rows;
+
+/* Norm and rotation in training.
+ *  q, q_out [n_tokens, n_heads], k, k_out [n_tokens, n_kv_heads] rows
+ *  positions int32 [n_axes, n_tokens] (device; NULL if rot_dim is 0)
+ * n_tokens below 2^31; 0 does nothing. */
+int proxy_qk_norm_rope_forward(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n_tokens,
+                               const pf_rows* q, const pf_rows* k, const int32_t* positions,
+                               const pf_rows* q_out, const pf_rows* k_out, void* stream);
+
+/* Its backward: dq and dk of the inputs q and k (with PF_NORM_NONE these are
+ * not read and may be NULL) from dq_out and dk_out, and the gains' gradients
+ * dgamma_q, dgamma_k [head_dim] fp32, overwritten, summed over tokens and
+ * heads in a fixed order (NULL: not computed; with PF_NORM_NONE not written).
+ * dq and dk may be dq_out's and dk_out's rows. n_tokens = 0 writes zero gain
+ * gradients. workspace: proxy_qk_workspace_size bytes (0 without a norm, or
+ * for an invalid config). */
+size_t proxy_qk_workspace_size(const pf_heads_config* cfg, int64_t n_tokens);
+int proxy_qk_norm_rope_backward(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n_tokens,
+                                const pf_rows* q, const pf_rows* k, const int32_t* positions,
+                                const pf_rows* dq_out, const pf_rows* dk_out, const pf_rows* dq,
+                                const pf_rows* dk, float* dgamma_q, float* dgamma_k, void* workspace,
+                                size_t ws_bytes, void* stream);
+
+/* A cache in pages, one of K and one of V per layer; everything on the device
+ * and the caller's own.
+ *  k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim]; page_size a
+ *  multiple of 16, n_pages * n_kv_heads * page_size below 2^31
+ *  page_table int32 [batch, max_pages]: page i of sequence b holds its rows
+ *  i * page_size ..; max_pages * page_size at most 2^31 - 65536. Entries past
+ *  a sequence's length are not read; an entry outside 0..n_pages-1 stands for
+ *  no page: nothing is written there, and its rows are not seen.
+ *  kv_len int32 [batch]: rows of every sequence, those of the tokens being
+ *  appended among them (one array serves a step's append and its attention in
+ *  every layer). 0 or less: an empty slot.
+ * Table and lengths are read on the device when the kernels run, so a captured
+ * graph follows their changes. */
+typedef struct {
+  void* k_pages;
+  void* v_pages;
+  int32_t n_pages, page_size;
+  const int32_t* page_table;
+  int32_t max_pages;
+  const int32_t* kv_len;
+  int32_t batch;
+} pf_paged_cache;
+
+/* New tokens into the cache: keys normed and turned, values as they are, and
+ * on the way the tokens' queries (q NULL: none; then q_out is not read).
+ *  q, q_out [n_tokens, n_heads], k, v [n_tokens, n_kv_heads] rows
+ *  cu_tokens int32 [batch + 1] (device), rising from 0: tokens
+ *  cu_tokens[b] .. cu_tokens[b + 1] - 1 are the last of sequence b, the i-th
+ *  of them its row kv_len[b] - (cu_tokens[b + 1] - cu_tokens[b]) + i. Tokens
+ *  behind the last sequence are left alone. NULL: one token of every sequence
+ *  (n_tokens = batch), its row kv_len[b] - 1.
+ *  positions int32 [n_axes, n_tokens], or NULL: every coordinate is the
+ *  token's row.
+ * A token whose row has no page (an empty slot, a row before 0 or past the
+ * table, an entry outside the cache) is left alone: neither cached nor its
+ * query written. k and v must not overlap the pages. */
+int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_cache* cache,
+                       int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
+                       const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream);
+
+/* Attention of new tokens over the cached rows that they see. The tokens are
+ * laid out as the append's: cu_tokens (device) tells which are whose, NULL
+ * stands for one token of every sequence (n_tokens = batch). A token whose row
+ * is r (as the append numbers them) sees the rows up to r: all of them, or
+ * with window > 0 the last `window` and the first `sinks` (ignored where
+ * window is 0). q [n_tokens, n_heads] rows, as the append gives them; out
+ * [n_tokens, n_heads, head_dim] contiguous, not overlapping q; lse fp32
+ * [n_tokens, n_heads] or NULL: log of the sum of exp(scale * q.k), to join the
+ * result with another attention's. A token that sees nothing (an empty slot):
+ * out is zero and lse -inf. Tokens behind the last sequence: out and lse are
+ * left as they were. The norm and the rotation of cfg are not applied here.
+ * A row that a token does not see has no weight in its result; of the rows
+ * that other tokens of the same call see it is taken times zero, so an
+ * infinity or a NaN in one of those can reach it.
+ *  max_new, max_kv_len (at least 1): most new tokens and rows of a sequence,
+ *  which the launch is laid out for; larger ones are right but slower. The
+ *  workspace goes by them.
+ *  workspace: proxy_paged_workspace_size bytes (`ragged`: whether cu_tokens is
+ *  given), aligned to 256; 0 when no sequence is cut, and for invalid sizes.
+ *  Calls that may run at the same time, graphs' replays among them, need
+ *  workspaces of their own.
+ * n_tokens * n_heads below 2^31; n_tokens = 0 does nothing. The result does
+ * not depend on where pages lie and is the same in every run. */
+size_t proxy_paged_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
+                                  int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks);
+int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cache, int64_t n_tokens,
+                          const int32_t* cu_tokens, const pf_rows* q, int64_t max_new, int64_t max_kv_len,
+                          int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace,
+                          size_t ws_bytes, void* stream);
+
 /* Launch tracing (profiling aid). While enabled, every kernel launch of the
  * library is bracketed by two HIP events recorded on its stream and
  * attributed to a label (e.g. "gate_gemm", "attention_fwd", "decode_attn").

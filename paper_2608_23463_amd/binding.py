@@ -30,6 +30,11 @@ PF_PRECISION_EXTENDED = 0
 PF_PRECISION_BF16 = 1
 PF_GATE_SEPARATE = 0
 PF_GATE_FUSED = 1
+MAX_AXES = 3
+PF_NORM_NONE = 0
+PF_NORM_RMS = 1
+PF_ROPE_HALVES = 0
+PF_ROPE_PAIRS = 1
 
 EXPORTS = (
     "proxy_layer_workspace_size", "proxy_layer_saved_size", "proxy_layer_forward",
@@ -38,6 +43,8 @@ EXPORTS = (
     "proxy_last_error", "proxy_version",
     "proxy_trace_enable", "proxy_trace_collect", "proxy_trace_get", "proxy_trace_reset",
     "proxy_ceiling_mfma", "proxy_decode_step_static", "proxy_ceiling_read",
+    "proxy_qk_norm_rope_forward", "proxy_qk_workspace_size", "proxy_qk_norm_rope_backward",
+    "proxy_paged_append", "proxy_paged_workspace_size", "proxy_paged_attention",
 )
 
 c_void_p = ctypes.c_void_p
@@ -89,6 +96,25 @@ class PfDecodeState(ctypes.Structure):
     _fields_ = [("k_cache", c_void_p), ("v_cache", c_void_p), ("n_cap", c_int64), ("n", c_int64),
                 ("x_blk", c_void_p), ("k_loc", c_void_p), ("v_loc", c_void_p), ("j", c_int32),
                 ("n_seq", ctypes.POINTER(c_int64)), ("j_seq", ctypes.POINTER(c_int32))]
+
+
+class PfHeadsConfig(ctypes.Structure):
+    _fields_ = [("n_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32), ("dtype", c_int32),
+                ("norm", c_int32), ("eps", ctypes.c_float), ("rot_dim", c_int32), ("rope_style", c_int32),
+                ("n_axes", c_int32), ("axis_pairs", c_int32 * MAX_AXES)]
+
+
+class PfHeadsWeights(ctypes.Structure):
+    _fields_ = [("gamma_q", c_void_p), ("gamma_k", c_void_p), ("freqs", c_void_p)]
+
+
+class PfRows(ctypes.Structure):
+    _fields_ = [("p", c_void_p), ("token_stride", c_int64), ("head_stride", c_int64)]
+
+
+class PfPagedCache(ctypes.Structure):
+    _fields_ = [("k_pages", c_void_p), ("v_pages", c_void_p), ("n_pages", c_int32), ("page_size", c_int32),
+                ("page_table", c_void_p), ("max_pages", c_int32), ("kv_len", c_void_p), ("batch", c_int32)]
 
 
 _lib = None
@@ -196,6 +222,26 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.proxy_decode_step_static.argtypes = [P(PfDecodeConfig), P(PfDecodeWeights), P(PfDecodeState), c_void_p,
                                              c_void_p, c_void_p]
     lib.proxy_decode_step_static.restype = c_int32
+    rows = P(PfRows)
+    lib.proxy_qk_norm_rope_forward.argtypes = [P(PfHeadsConfig), P(PfHeadsWeights), c_int64, rows, rows, c_void_p,
+                                               rows, rows, c_void_p]
+    lib.proxy_qk_norm_rope_forward.restype = c_int32
+    lib.proxy_qk_workspace_size.argtypes = [P(PfHeadsConfig), c_int64]
+    lib.proxy_qk_workspace_size.restype = c_size_t
+    lib.proxy_qk_norm_rope_backward.argtypes = [P(PfHeadsConfig), P(PfHeadsWeights), c_int64, rows, rows, c_void_p,
+                                                rows, rows, rows, rows, c_void_p, c_void_p, c_void_p, c_size_t,
+                                                c_void_p]
+    lib.proxy_qk_norm_rope_backward.restype = c_int32
+    lib.proxy_paged_append.argtypes = [P(PfHeadsConfig), P(PfHeadsWeights), P(PfPagedCache), c_int64, c_void_p, rows,
+                                       rows, rows, c_void_p, rows, c_void_p]
+    lib.proxy_paged_append.restype = c_int32
+    lib.proxy_paged_workspace_size.argtypes = [P(PfHeadsConfig), c_int32, c_int64, c_int32, c_int64, c_int64, c_int64,
+                                               c_int64]
+    lib.proxy_paged_workspace_size.restype = c_size_t
+    lib.proxy_paged_attention.argtypes = [P(PfHeadsConfig), P(PfPagedCache), c_int64, c_void_p, rows, c_int64, c_int64,
+                                          c_int64, c_int64, ctypes.c_float, c_void_p, c_void_p, c_void_p, c_size_t,
+                                          c_void_p]
+    lib.proxy_paged_attention.restype = c_int32
     _lib = lib
     return lib
 
@@ -517,3 +563,253 @@ class DecodeSession:
         _check(load().proxy_cache_append(ctypes.byref(self.cfg), ctypes.byref(self.wstruct),
                                          ctypes.byref(self.state), _ptr(x_blocks), nblk,
                                          _ptr(self.workspace), self.workspace.numel(), _stream(stream)))
+
+
+# ---------------------------------------------------------------- heads
+
+def heads_config(n_heads: int, n_kv_heads: int, head_dim: int, dtype: str = "bf16", norm: bool = True,
+                 eps: float = 1e-6, rot_dim: Optional[int] = None, style: int = PF_ROPE_HALVES,
+                 axis_pairs: Sequence[int] = ()) -> PfHeadsConfig:
+    """Heads of the fine tokens' own attention. rot_dim: elements that are
+    turned (all of head_dim unless given); axis_pairs: pairs that turn by each
+    coordinate of a position (one coordinate unless given)."""
+    if dtype not in ("bf16", "fp32"):
+        raise ValueError("dtype must be 'bf16' or 'fp32'")
+    if len(axis_pairs) > MAX_AXES:
+        raise ValueError(f"at most {MAX_AXES} axes")
+    c = PfHeadsConfig()
+    c.n_heads = n_heads
+    c.n_kv_heads = n_kv_heads
+    c.head_dim = head_dim
+    c.dtype = PF_BF16 if dtype == "bf16" else PF_FP32
+    c.norm = PF_NORM_RMS if norm else PF_NORM_NONE
+    c.eps = eps
+    c.rot_dim = head_dim if rot_dim is None else rot_dim
+    c.rope_style = style
+    pairs = list(axis_pairs) if len(axis_pairs) else [c.rot_dim // 2]
+    c.n_axes = len(pairs)
+    for i, n in enumerate(pairs):
+        c.axis_pairs[i] = n
+    return c
+
+
+def rope_freqs(cfg: PfHeadsConfig, base: float = 10000.0, device="cuda"):
+    """freqs [rot_dim / 2] fp64: base ** (-p / n) for pair p of an axis' n pairs."""
+    import torch
+    return torch.cat([base ** (-torch.arange(n, dtype=torch.float64) / max(n, 1))
+                      for n in cfg.axis_pairs[:cfg.n_axes]]).to(device)
+
+
+def _heads_dtype(cfg):
+    import torch
+    return torch.bfloat16 if cfg.dtype == PF_BF16 else torch.float32
+
+
+def _want(name, t, dtype, device, shape, contiguous=True):
+    """A device tensor of a call: type, place and shape (None: any size)."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device or not t.is_cuda:
+        raise ValueError(f"{name} must be on the call's GPU {device}, got {t.device}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _rows(cfg, name, t, n, heads, device) -> PfRows:
+    """The rows of a tensor [tokens, heads, head_dim]; only a row itself must be contiguous."""
+    p = _want(name, t, _heads_dtype(cfg), device, (n, heads, cfg.head_dim), contiguous=False)
+    ts, hs, es = t.stride()
+    if es != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    return PfRows(p, ts if n > 1 else 0, hs if heads > 1 else 0)
+
+
+def _heads_weights(cfg, weights: Dict[str, object], device) -> PfHeadsWeights:
+    import torch
+    s = PfHeadsWeights()
+    for name in ("gamma_q", "gamma_k"):
+        t = weights.get(name)
+        if t is not None:
+            setattr(s, name, _want(name, t, _heads_dtype(cfg), device, (cfg.head_dim,)))
+    t = weights.get("freqs")
+    if t is not None:
+        s.freqs = _want("freqs", t, torch.float64, device, (cfg.rot_dim // 2,))
+    return s
+
+
+def _positions(cfg, positions, n, device):
+    import torch
+    if positions is None:
+        return None
+    if positions.dim() == 1:
+        positions = positions[None]
+    return _want("positions", positions, torch.int32, device, (cfg.n_axes, n))
+
+
+class _On:
+    """The call's GPU as the current one, with `stream` (None: its current
+    stream) as the one that buffers are allocated on and kernels launched to."""
+
+    def __init__(self, device, stream):
+        import torch
+        if device.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU, got {device}")
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
+        self.ctx = torch.cuda.stream(stream) if stream is not None else None
+        if self.ctx is None and device.index != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(device)
+        self.device = device
+
+    def __enter__(self):
+        import torch
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def qk_norm_rope_forward(cfg: PfHeadsConfig, weights: Dict[str, object], q, k, positions=None, q_out=None, k_out=None,
+                         stream=None):
+    """Queries [T, n_heads, head_dim] and keys [T, n_kv_heads, head_dim]
+    normed per head and turned by positions (int32 [n_axes, T] or [T]);
+    weights {"gamma_q", "gamma_k", "freqs"}. Returns (q_out, k_out)."""
+    dev, n = q.device, q.shape[0]
+    with _On(dev, stream) as s:
+        w = _heads_weights(cfg, weights, dev)
+        rq, rk = _rows(cfg, "q", q, n, cfg.n_heads, dev), _rows(cfg, "k", k, n, cfg.n_kv_heads, dev)
+        at = _positions(cfg, positions, n, dev)
+        if q_out is None:
+            q_out = _empty(q.shape, q.dtype, dev)
+        if k_out is None:
+            k_out = _empty(k.shape, k.dtype, dev)
+        ro, rp = _rows(cfg, "q_out", q_out, n, cfg.n_heads, dev), _rows(cfg, "k_out", k_out, n, cfg.n_kv_heads, dev)
+        _check(load().proxy_qk_norm_rope_forward(ctypes.byref(cfg), ctypes.byref(w), n, ctypes.byref(rq),
+                                                 ctypes.byref(rk), at, ctypes.byref(ro), ctypes.byref(rp), s))
+    return q_out, k_out
+
+
+def qk_norm_rope_backward(cfg: PfHeadsConfig, weights: Dict[str, object], q, k, positions, dq_out, dk_out, dq=None,
+                          dk=None, workspace=None, stream=None):
+    """Gradients of qk_norm_rope_forward's q and k (of their dtype) and of the
+    gains (fp32; None without a norm). q and k are the forward's inputs."""
+    import torch
+    dev, n = dq_out.device, dq_out.shape[0]
+    norm = cfg.norm == PF_NORM_RMS
+    with _On(dev, stream) as s:
+        lib = load()
+        w = _heads_weights(cfg, weights, dev)
+        if norm:
+            rq, rk = _rows(cfg, "q", q, n, cfg.n_heads, dev), _rows(cfg, "k", k, n, cfg.n_kv_heads, dev)
+        else:
+            rq = rk = PfRows(None, 0, 0)
+        at = _positions(cfg, positions, n, dev)
+        ro = _rows(cfg, "dq_out", dq_out, n, cfg.n_heads, dev)
+        rp = _rows(cfg, "dk_out", dk_out, n, cfg.n_kv_heads, dev)
+        if dq is None:
+            dq = _empty(dq_out.shape, dq_out.dtype, dev)
+        if dk is None:
+            dk = _empty(dk_out.shape, dk_out.dtype, dev)
+        gq = gk = None
+        ws, ws_bytes = None, 0
+        if norm:
+            gains = _empty((2, cfg.head_dim), torch.float32, dev)
+            gq, gk = gains[0], gains[1]
+            ws_bytes = int(lib.proxy_qk_workspace_size(ctypes.byref(cfg), n))
+            if workspace is None:
+                workspace = _bytes(ws_bytes, dev)
+            ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        da, db = _rows(cfg, "dq", dq, n, cfg.n_heads, dev), _rows(cfg, "dk", dk, n, cfg.n_kv_heads, dev)
+        _check(lib.proxy_qk_norm_rope_backward(ctypes.byref(cfg), ctypes.byref(w), n, ctypes.byref(rq),
+                                               ctypes.byref(rk), at, ctypes.byref(ro), ctypes.byref(rp),
+                                               ctypes.byref(da), ctypes.byref(db), _ptr(gq), _ptr(gk), ws, ws_bytes, s))
+    return dq, dk, gq, gk
+
+
+class PagedCache:
+    """A cache of the fine tokens' keys and values in pages (one per layer).
+
+    k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim]; page_table
+    int32 [batch, max_pages] and kv_len int32 [batch] on the device, the
+    caller's own: it hands out pages and sets kv_len (the new tokens counted)
+    before a step's append, and the step's attention reads the same lengths."""
+
+    def __init__(self, cfg: PfHeadsConfig, weights: Dict[str, object], k_pages, v_pages, page_table, kv_len):
+        import torch
+        dev, dt = k_pages.device, _heads_dtype(cfg)
+        shape = (k_pages.shape[0], cfg.n_kv_heads, None, cfg.head_dim)
+        batch = kv_len.shape[0]
+        self.cfg = cfg
+        self.device = dev
+        self.tensors = (k_pages, v_pages, page_table, kv_len, weights)  # kept alive
+        self.batch = batch
+        self.wstruct = _heads_weights(cfg, weights, dev)
+        self.state = PfPagedCache(_want("k_pages", k_pages, dt, dev, shape),
+                                  _want("v_pages", v_pages, dt, dev, tuple(k_pages.shape)), k_pages.shape[0],
+                                  k_pages.shape[2], _want("page_table", page_table, torch.int32, dev, (batch, None)),
+                                  page_table.shape[1], _want("kv_len", kv_len, torch.int32, dev, (batch,)), batch)
+
+    def append(self, k, v, q=None, cu_tokens=None, positions=None, q_out=None, stream=None):
+        """New tokens' keys and values [T, n_kv_heads, head_dim] into the pages,
+        and their queries [T, n_heads, head_dim] normed and turned into q_out
+        (returned). cu_tokens int32 [batch + 1]: which tokens are whose (None:
+        one of every sequence); positions as in qk_norm_rope_forward (None:
+        the tokens' rows). Tokens without a place are left alone: pass a
+        q_out of your own where that can be."""
+        import torch
+        cfg, dev, n = self.cfg, self.device, k.shape[0]
+        with _On(dev, stream) as s:
+            rk, rv = _rows(cfg, "k", k, n, cfg.n_kv_heads, dev), _rows(cfg, "v", v, n, cfg.n_kv_heads, dev)
+            cu = None if cu_tokens is None else _want("cu_tokens", cu_tokens, torch.int32, dev, (self.batch + 1,))
+            at = _positions(cfg, positions, n, dev)
+            rq = ro = None
+            if q is not None:
+                rq = _rows(cfg, "q", q, n, cfg.n_heads, dev)
+                if q_out is None:
+                    q_out = _empty(q.shape, q.dtype, dev)
+                ro = _rows(cfg, "q_out", q_out, n, cfg.n_heads, dev)
+            elif q_out is not None:
+                raise ValueError("q_out without q")
+            _check(load().proxy_paged_append(ctypes.byref(cfg), ctypes.byref(self.wstruct), ctypes.byref(self.state),
+                                             n, cu, rq, ctypes.byref(rk), ctypes.byref(rv), at, ro, s))
+        return q_out
+
+    def attend(self, q, max_kv_len: int, cu_tokens=None, max_new: Optional[int] = None, window: int = 0,
+               sinks: int = 0, scale: Optional[float] = None, out=None, lse=None, workspace=None, stream=None):
+        """Attention of new tokens, q [T, n_heads, head_dim] laid out as append's,
+        over the rows up to their own: all of them, or (window > 0) the last
+        `window` and the first `sinks`. max_kv_len, max_new: most rows and new
+        tokens of a sequence, to lay the launch out for (max_new: 1 without
+        cu_tokens, T with it unless given). scale: 1 / sqrt(head_dim) unless
+        given. lse: an fp32 [T, n_heads] tensor for the log-sums. Returns out;
+        rows of tokens behind the last sequence are left alone."""
+        import torch
+        cfg, dev, n = self.cfg, self.device, q.shape[0]
+        if max_new is None:
+            max_new = 1 if cu_tokens is None else max(n, 1)
+        with _On(dev, stream) as s:
+            lib = load()
+            rq = _rows(cfg, "q", q, n, cfg.n_heads, dev)
+            cu = None if cu_tokens is None else _want("cu_tokens", cu_tokens, torch.int32, dev, (self.batch + 1,))
+            shape = (n, cfg.n_heads, cfg.head_dim)
+            if out is None:
+                out = _empty(shape, q.dtype, dev)
+            to = _want("out", out, q.dtype, dev, shape)
+            tl = None if lse is None else _want("lse", lse, torch.float32, dev, (n, cfg.n_heads))
+            if workspace is None:
+                need = int(lib.proxy_paged_workspace_size(ctypes.byref(cfg), self.batch, n, cu is not None, max_new,
+                                                          max_kv_len, window, sinks))
+                workspace = _bytes(need, dev) if need else None
+            ws, ws_bytes = None, 0
+            if workspace is not None:
+                ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+            _check(lib.proxy_paged_attention(ctypes.byref(cfg), ctypes.byref(self.state), n, cu, rq, max_new,
+                                             max_kv_len, window, sinks,
+                                             cfg.head_dim ** -0.5 if scale is None else scale, to, tl, ws, ws_bytes, s))
+        return out

@@ -2,6 +2,7 @@
 // dtype-specific launch sequences. Nothing is enqueued unless every check
 // passes.
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -11,6 +12,7 @@
 #include "ceiling.hpp"
 #include "common.hpp"
 #include "decode.hpp"
+#include "heads.hpp"
 #include "layer.hpp"
 
 namespace pf {
@@ -449,6 +451,266 @@ int proxy_cache_append(const pf_decode_config* cfg, const pf_decode_weights* w, 
     st->n += nblk;
   }
   return PF_OK;
+}
+
+// ---------------------------------------------------------------- heads
+
+// Rows of a call: `n` tokens of `heads` heads. Writable rows share no element.
+static int check_rows(const char* name, const pf_rows* r, int64_t n, int heads, const HeadsDims& d, bool written) {
+  if (!r || !r->p) return fail(PF_ERR_INVALID_ARG, "%s is NULL", name);
+  const int64_t ts = r->token_stride, hs = r->head_stride;
+  if (ts < 0 || hs < 0) return fail(PF_ERR_INVALID_ARG, "%s: strides must not be negative", name);
+  if (!aligned16(r->p) || (ts * d.esize) % 16 != 0 || (hs * d.esize) % 16 != 0)
+    return fail(PF_ERR_INVALID_ARG, "%s: rows must be 16-byte aligned", name);
+  const int64_t most = (int64_t)1 << 59;  // elements, so that byte offsets stay in 64 bits
+  if ((n > 1 && ts > most / (n - 1)) || (heads > 1 && hs > most / (heads - 1)))
+    return fail(PF_ERR_INVALID_ARG, "%s: strides too large", name);
+  if (!written) return PF_OK;
+  const int64_t across = (heads - 1) * hs + d.d, along = (n - 1) * ts + d.d;  // one token's heads, one head's tokens
+  const bool tokens_apart = (heads == 1 || hs >= d.d) && (n == 1 || ts >= across);
+  const bool heads_apart = (n == 1 || ts >= d.d) && (heads == 1 || hs >= along);
+  if (!tokens_apart && !heads_apart) return fail(PF_ERR_INVALID_ARG, "%s: rows overlap each other", name);
+  return PF_OK;
+}
+
+static Rows rows_of(const pf_rows* r) {
+  Rows o;
+  if (r) {
+    o.p = static_cast<char*>(r->p);
+    o.ts = r->token_stride;
+    o.hs = r->head_stride;
+  }
+  return o;
+}
+
+static size_t rows_bytes(const pf_rows& r, int64_t n, int heads, const HeadsDims& d) {
+  return (size_t)((n - 1) * r.token_stride + (heads - 1) * r.head_stride + d.d) * d.esize;
+}
+
+// Whether two sets of rows may share elements. Bands of one buffer with the
+// same stride (the slices of a fused projection) are told apart within a
+// period of that stride; everything else by its whole extent.
+static bool rows_meet(const pf_rows& a, int ha, const pf_rows& b, int hb, int64_t n, const HeadsDims& d) {
+  if (!overlaps(a.p, rows_bytes(a, n, ha, d), b.p, rows_bytes(b, n, hb, d))) return false;
+  const int64_t delta = (reinterpret_cast<intptr_t>(b.p) - reinterpret_cast<intptr_t>(a.p)) / d.esize;
+  auto apart = [&](int64_t period, int64_t wa, int64_t wb) {
+    if (period <= 0 || wa > period || wb > period) return false;
+    const int64_t at = ((delta % period) + period) % period;
+    return at >= wa && at + wb <= period;
+  };
+  if (a.token_stride == b.token_stride &&
+      apart(a.token_stride, (ha - 1) * a.head_stride + d.d, (hb - 1) * b.head_stride + d.d))
+    return false;
+  if (a.head_stride == b.head_stride &&
+      apart(a.head_stride, (n - 1) * a.token_stride + d.d, (n - 1) * b.token_stride + d.d))
+    return false;
+  return true;
+}
+
+static bool same_rows(const pf_rows& a, const pf_rows& b) {
+  return a.p == b.p && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
+}
+
+static int check_heads(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n, HeadsDims* d,
+                       HeadsWeights* hw) {
+  const char* why;
+  const int st = heads_dims(cfg, d, &why);
+  if (st != PF_OK) return fail(st, "invalid heads config: %s", why);
+  if (!w) return fail(PF_ERR_INVALID_ARG, "weights struct is NULL");
+  if (n < 0) return fail(PF_ERR_INVALID_ARG, "n_tokens must be >= 0");
+  if (n > INT32_MAX) return fail(PF_ERR_UNSUPPORTED, "n_tokens above 2^31 - 1");
+  if (d->norm && (!aligned16(w->gamma_q) || !aligned16(w->gamma_k)))
+    return fail(PF_ERR_INVALID_ARG, "gains must be 16-byte aligned");
+  if (d->rot && !w->freqs) return fail(PF_ERR_INVALID_ARG, "freqs is NULL");
+  if (reinterpret_cast<uintptr_t>(w->freqs) & 7) return fail(PF_ERR_INVALID_ARG, "freqs must be 8-byte aligned");
+  *hw = HeadsWeights{w->gamma_q, w->gamma_k, w->freqs};
+  return PF_OK;
+}
+
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+
+int proxy_qk_norm_rope_forward(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n_tokens,
+                               const pf_rows* q, const pf_rows* k, const int32_t* positions, const pf_rows* q_out,
+                               const pf_rows* k_out, void* stream) {
+  HeadsDims d;
+  HeadsWeights hw;
+  int st = check_heads(cfg, w, n_tokens, &d, &hw);
+  if (st != PF_OK) return st;
+  if (n_tokens == 0) return PF_OK;
+  if ((st = check_rows("q", q, n_tokens, d.hq, d, false)) != PF_OK) return st;
+  if ((st = check_rows("k", k, n_tokens, d.hk, d, false)) != PF_OK) return st;
+  if ((st = check_rows("q_out", q_out, n_tokens, d.hq, d, true)) != PF_OK) return st;
+  if ((st = check_rows("k_out", k_out, n_tokens, d.hk, d, true)) != PF_OK) return st;
+  if (d.rot && !positions) return fail(PF_ERR_INVALID_ARG, "positions is NULL");
+  if (!aligned4(positions)) return fail(PF_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+  const int64_t n = n_tokens;
+  if ((!same_rows(*q, *q_out) && rows_meet(*q, d.hq, *q_out, d.hq, n, d)) ||
+      (!same_rows(*k, *k_out) && rows_meet(*k, d.hk, *k_out, d.hk, n, d)) ||
+      rows_meet(*k, d.hk, *q_out, d.hq, n, d) || rows_meet(*q, d.hq, *k_out, d.hk, n, d) ||
+      rows_meet(*q_out, d.hq, *k_out, d.hk, n, d))
+    return fail(PF_ERR_INVALID_ARG, "q_out and k_out must not overlap other rows of the call");
+  return hip_status(launch_qk_forward(d, hw, n, rows_of(q), rows_of(k), positions, rows_of(q_out), rows_of(k_out),
+                                      reinterpret_cast<hipStream_t>(stream)),
+                    "proxy_qk_norm_rope_forward launch");
+}
+
+size_t proxy_qk_workspace_size(const pf_heads_config* cfg, int64_t n_tokens) {
+  HeadsDims d;
+  const char* why;
+  if (heads_dims(cfg, &d, &why) != PF_OK || n_tokens < 0 || n_tokens > INT32_MAX) return 0;
+  return qk_backward_ws(d, n_tokens);
+}
+
+int proxy_qk_norm_rope_backward(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n_tokens,
+                                const pf_rows* q, const pf_rows* k, const int32_t* positions, const pf_rows* dq_out,
+                                const pf_rows* dk_out, const pf_rows* dq, const pf_rows* dk, float* dgamma_q,
+                                float* dgamma_k, void* workspace, size_t ws_bytes, void* stream) {
+  HeadsDims d;
+  HeadsWeights hw;
+  int st = check_heads(cfg, w, n_tokens, &d, &hw);
+  if (st != PF_OK) return st;
+  if (!aligned4(dgamma_q) || !aligned4(dgamma_k))
+    return fail(PF_ERR_INVALID_ARG, "gain gradients must be 4-byte aligned");
+  const int64_t n = n_tokens;
+  if (n > 0) {
+    if (d.norm) {
+      if ((st = check_rows("q", q, n, d.hq, d, false)) != PF_OK) return st;
+      if ((st = check_rows("k", k, n, d.hk, d, false)) != PF_OK) return st;
+    }
+    if ((st = check_rows("dq_out", dq_out, n, d.hq, d, false)) != PF_OK) return st;
+    if ((st = check_rows("dk_out", dk_out, n, d.hk, d, false)) != PF_OK) return st;
+    if ((st = check_rows("dq", dq, n, d.hq, d, true)) != PF_OK) return st;
+    if ((st = check_rows("dk", dk, n, d.hk, d, true)) != PF_OK) return st;
+    if (d.rot && !positions) return fail(PF_ERR_INVALID_ARG, "positions is NULL");
+    if (!aligned4(positions)) return fail(PF_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+    const pf_rows* in[4] = {dq_out, dk_out, d.norm ? q : nullptr, d.norm ? k : nullptr};
+    for (int i = 0; i < 4; ++i) {
+      if (!in[i]) continue;
+      const int h = i % 2 ? d.hk : d.hq;  // dq may be its own inputs' rows, and dk its
+      if ((!(i % 2 == 0 && same_rows(*in[i], *dq)) && rows_meet(*in[i], h, *dq, d.hq, n, d)) ||
+          (!(i % 2 == 1 && same_rows(*in[i], *dk)) && rows_meet(*in[i], h, *dk, d.hk, n, d)))
+        return fail(PF_ERR_INVALID_ARG, "dq and dk must not overlap other rows of the call");
+    }
+    if (rows_meet(*dq, d.hq, *dk, d.hk, n, d)) return fail(PF_ERR_INVALID_ARG, "dq and dk must not overlap");
+  }
+  const size_t need = qk_backward_ws(d, n);
+  if (need && (dgamma_q || dgamma_k)) {
+    if (!workspace || ws_bytes < need)
+      return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need, workspace ? ws_bytes : 0);
+    if (!aligned16(workspace)) return fail(PF_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  }
+  return hip_status(launch_qk_backward(d, hw, n, rows_of(q), rows_of(k), positions, rows_of(dq_out), rows_of(dk_out),
+                                       rows_of(dq), rows_of(dk), dgamma_q, dgamma_k, static_cast<float*>(workspace),
+                                       reinterpret_cast<hipStream_t>(stream)),
+                    "proxy_qk_norm_rope_backward launch");
+}
+
+static int check_paged(const pf_paged_cache* c, const HeadsDims& d, PagedDims* o) {
+  if (!c) return fail(PF_ERR_INVALID_ARG, "cache is NULL");
+  if (!c->k_pages || !c->v_pages || !c->page_table || !c->kv_len)
+    return fail(PF_ERR_INVALID_ARG, "k_pages, v_pages, page_table and kv_len must be non-NULL");
+  if (!aligned16(c->k_pages) || !aligned16(c->v_pages))
+    return fail(PF_ERR_INVALID_ARG, "pages must be 16-byte aligned");
+  if (!aligned4(c->page_table) || !aligned4(c->kv_len))
+    return fail(PF_ERR_INVALID_ARG, "page_table and kv_len must be 4-byte aligned");
+  if (c->batch < 1 || c->n_pages < 1 || c->max_pages < 1 || c->page_size < 1)
+    return fail(PF_ERR_INVALID_ARG, "batch, n_pages, max_pages and page_size must be >= 1");
+  if (c->page_size % 16 != 0) return fail(PF_ERR_UNSUPPORTED, "page_size must be a multiple of 16");
+  if ((int64_t)c->max_pages * c->page_size > INT32_MAX - 65535)
+    return fail(PF_ERR_UNSUPPORTED, "max_pages * page_size above 2^31 - 65536");
+  if ((__int128)c->n_pages * d.hk * c->page_size > INT32_MAX)
+    return fail(PF_ERR_UNSUPPORTED, "n_pages * n_kv_heads * page_size above 2^31 - 1");
+  const size_t bytes = (size_t)c->n_pages * d.hk * c->page_size * d.d * d.esize;
+  if (overlaps(c->k_pages, bytes, c->v_pages, bytes))
+    return fail(PF_ERR_INVALID_ARG, "k_pages and v_pages must not overlap");
+  *o = PagedDims{static_cast<char*>(c->k_pages), static_cast<char*>(c->v_pages), c->n_pages, c->page_size,
+                 c->page_table, c->max_pages, c->kv_len, c->batch};
+  return PF_OK;
+}
+
+int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_cache* cache,
+                       int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
+                       const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream) {
+  HeadsDims d;
+  HeadsWeights hw;
+  PagedDims c;
+  int st = check_heads(cfg, w, n_tokens, &d, &hw);
+  if (st != PF_OK) return st;
+  if ((st = check_paged(cache, d, &c)) != PF_OK) return st;
+  if (!cu_tokens && n_tokens != c.batch)
+    return fail(PF_ERR_INVALID_ARG, "without cu_tokens n_tokens must be batch: one token of every sequence");
+  if (!aligned4(cu_tokens) || !aligned4(positions))
+    return fail(PF_ERR_INVALID_ARG, "cu_tokens and positions must be 4-byte aligned");
+  if (n_tokens == 0) return PF_OK;
+  const int64_t n = n_tokens;
+  const bool with_q = q && q->p;
+  if ((st = check_rows("k", k, n, d.hk, d, false)) != PF_OK) return st;
+  if ((st = check_rows("v", v, n, d.hk, d, false)) != PF_OK) return st;
+  const size_t pages = (size_t)c.n_pages * d.hk * c.page_size * d.d * d.esize;
+  auto on_pages = [&](const pf_rows* r, int heads) {
+    const size_t bytes = rows_bytes(*r, n, heads, d);
+    return overlaps(r->p, bytes, c.k, pages) || overlaps(r->p, bytes, c.v, pages);
+  };
+  if (with_q) {
+    if ((st = check_rows("q", q, n, d.hq, d, false)) != PF_OK) return st;
+    if ((st = check_rows("q_out", q_out, n, d.hq, d, true)) != PF_OK) return st;
+    if ((!same_rows(*q, *q_out) && rows_meet(*q, d.hq, *q_out, d.hq, n, d)) ||
+        rows_meet(*k, d.hk, *q_out, d.hq, n, d) || rows_meet(*v, d.hk, *q_out, d.hq, n, d))
+      return fail(PF_ERR_INVALID_ARG, "q_out must not overlap other rows of the call");
+    if (on_pages(q, d.hq) || on_pages(q_out, d.hq)) return fail(PF_ERR_INVALID_ARG, "q and q_out must not overlap the pages");
+  }
+  if (on_pages(k, d.hk) || on_pages(v, d.hk)) return fail(PF_ERR_INVALID_ARG, "k and v must not overlap the pages");
+  return hip_status(launch_paged_append(d, hw, c, n, cu_tokens, with_q ? rows_of(q) : Rows{}, rows_of(k), rows_of(v),
+                                        positions, with_q ? rows_of(q_out) : Rows{},
+                                        reinterpret_cast<hipStream_t>(stream)),
+                    "proxy_paged_append launch");
+}
+
+size_t proxy_paged_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
+                                  int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks) {
+  HeadsDims d;
+  const char* why;
+  if (heads_dims(cfg, &d, &why) != PF_OK || batch < 1 || n_tokens < 1 || n_tokens > INT32_MAX || max_new < 1 ||
+      max_kv_len < 1 || window < 0 || sinks < 0)
+    return 0;
+  return paged_plan(d, batch, n_tokens, ragged != 0, max_kv_len, window, sinks).bytes;
+}
+
+int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cache, int64_t n_tokens,
+                          const int32_t* cu_tokens, const pf_rows* q, int64_t max_new, int64_t max_kv_len,
+                          int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace,
+                          size_t ws_bytes, void* stream) {
+  HeadsDims d;
+  PagedDims c;
+  const char* why;
+  int st = heads_dims(cfg, &d, &why);
+  if (st != PF_OK) return fail(st, "invalid heads config: %s", why);
+  if ((st = check_paged(cache, d, &c)) != PF_OK) return st;
+  if (n_tokens < 0) return fail(PF_ERR_INVALID_ARG, "n_tokens must be >= 0");
+  if (!cu_tokens && n_tokens != c.batch)
+    return fail(PF_ERR_INVALID_ARG, "without cu_tokens n_tokens must be batch: one token of every sequence");
+  if (!aligned4(cu_tokens)) return fail(PF_ERR_INVALID_ARG, "cu_tokens must be 4-byte aligned");
+  if (max_new < 1 || max_kv_len < 1) return fail(PF_ERR_INVALID_ARG, "max_new and max_kv_len must be >= 1");
+  if (window < 0 || sinks < 0) return fail(PF_ERR_INVALID_ARG, "window and sinks must be >= 0");
+  if (!std::isfinite(scale)) return fail(PF_ERR_INVALID_ARG, "scale must be finite");
+  if (n_tokens == 0) return PF_OK;
+  if (n_tokens > INT32_MAX / d.hq) return fail(PF_ERR_UNSUPPORTED, "n_tokens * n_heads above 2^31 - 1");
+  const int64_t n = n_tokens;
+  if ((st = check_rows("q", q, n, d.hq, d, false)) != PF_OK) return st;
+  if (!out) return fail(PF_ERR_INVALID_ARG, "out is NULL");
+  if (!aligned16(out)) return fail(PF_ERR_INVALID_ARG, "out must be 16-byte aligned");
+  if (!aligned4(lse)) return fail(PF_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+  const size_t out_bytes = (size_t)n * d.hq * d.d * d.esize;
+  if (overlaps(out, out_bytes, q->p, rows_bytes(*q, n, d.hq, d)))
+    return fail(PF_ERR_INVALID_ARG, "out must not overlap q");
+  const PagedPlan pl = paged_plan(d, c.batch, n, cu_tokens != nullptr, max_kv_len, window, sinks);
+  if (pl.groups > INT32_MAX / pl.slices) return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes");
+  if (pl.bytes && (!workspace || ws_bytes < pl.bytes))
+    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", pl.bytes, workspace ? ws_bytes : 0);
+  if (!aligned16(workspace)) return fail(PF_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  return hip_status(launch_paged_attention(d, c, pl, n, cu_tokens, rows_of(q), scale, window, sinks, out, lse,
+                                           static_cast<char*>(workspace), reinterpret_cast<hipStream_t>(stream)),
+                    "proxy_paged_attention launch");
 }
 
 }  // extern "C"

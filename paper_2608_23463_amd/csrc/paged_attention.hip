@@ -1,0 +1,578 @@
+// Attention of new tokens, one of every sequence or a prompt, over a paged
+// cache.
+//
+//   o = sum_j softmax_j(scale q.k_j) v_j over the rows j that a token at row r
+//   of its sequence sees: j <= r and, with a window, j > r - window or j < sinks.
+//
+// paged_attention_kernel: tokens one by one are bound by HBM, every visible
+// row of K and V read once and 4 D flops per query head and row against 2 D
+// elements of a group of heads. The 16 columns of its matrix instructions are
+// the queries that share K and V: the heads of a group, and tokens after one
+// another where a group has fewer than 16. A row is fetched once for all of
+// them, and the multiplications cost next to nothing beside the loads, however
+// few of the columns are used. A (block of columns, K/V head, slice of the
+// rows) is a workgroup; its four waves take tiles of 16 * NB rows in turn and
+// each keeps its own running maximum and sum.
+//
+// Nothing passes through LDS on the way. The order in which a matrix
+// instruction's k index runs is free as long as both operands agree, and so is
+// the order of its m index as long as the results are stored by it:
+//  - scores: S^T[row, column] = K Q^T, lane (m, g) = (lane % 16, lane / 16)
+//    holds 16 bytes of K row m. The result leaves lane (n, g) with rows
+//    4 g .. 4 g + 3 of every block of 16 for column n.
+//  - values: O^T[d, column] += V^T P^T takes those rows in just that order as
+//    its k index, so the probabilities are an operand where they were computed.
+//    Lane (m, g) loads VE neighbouring channels VE m .. of the same rows, and
+//    the e-th instruction takes channel e of every lane: its m index stands for
+//    channel VE m + e. In bf16 one permute joins two rows of a channel.
+#include <algorithm>
+
+#include "heads.hpp"
+#include "trace.hpp"
+
+namespace pf {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kBlock = 16;      // rows per block: a page is a multiple of it
+constexpr int kCols = 16;       // queries of a workgroup
+constexpr int kMaxSlices = 512;
+
+struct PagedParams {
+  const char* q;
+  int64_t q_ts, q_hs;
+  const char* k;
+  const char* v;
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* cu;    // NULL: one token of every sequence
+  int n_pages, page_size, max_pages, batch, n_tokens;
+  FastDiv page_blocks;  // blocks per page
+  int hq, hk, group;
+  FastDiv fgroup, fhk, fslices;
+  int slices, min_tiles;
+  int window, sinks;    // window: INT32_MAX without one
+  float scale_log2;
+  void* out;
+  float* lse;
+  float* part_o;        // [n_tokens * hq, slices, D]
+  float2* part_ml;      // [n_tokens * hq, slices]
+};
+
+// The new tokens of one sequence. Column x of a (sequence, K/V head) is token
+// x / group, head x % group of the group.
+struct Sequence {
+  int seq;       // -1: none
+  int t0;        // its first token in the call
+  int cols;
+  int row0;      // row of that token
+  int most;      // rows that the table holds
+  __device__ __forceinline__ void set(const PagedParams& p, int s) {
+    seq = s;
+    int n_new = 1;
+    t0 = s;
+    if (p.cu) {
+      t0 = p.cu[s];
+      n_new = p.cu[s + 1] - t0;
+      if (t0 < 0 || n_new <= 0 || n_new > p.n_tokens - t0) {  // nothing there, or boundaries that are none
+        seq = -1;
+        n_new = 0;
+      }
+    }
+    cols = n_new * p.group;
+    const int64_t first = (int64_t)p.kv_len[s] - n_new;
+    row0 = (int)(first < -n_new ? -n_new : first);
+    most = p.max_pages * p.page_size;
+  }
+};
+
+// Sequence s takes blocks cu[s] * group / 16 + s on, at least as many as its
+// columns fill, so a block finds its sequence without a sum over the others.
+__device__ __forceinline__ int first_block(const PagedParams& p, int s) {
+  return p.cu ? (int)((int64_t)p.cu[s] * p.group / kCols) + s : s * ((p.group + kCols - 1) / kCols);
+}
+
+// The largest s < batch with at(s) <= x, counted by the wave, 64 at a time
+// (at rises with s, at(0) <= x).
+template <class F>
+__device__ __forceinline__ int find_sequence(int batch, F&& at, int64_t x) {
+  int s = 0;
+  for (int i = 1; i < batch; i += kWave) {
+    const int c = i + (int)(threadIdx.x & (kWave - 1));
+    s += __popcll(__ballot(c < batch && at(c < batch ? c : 0) <= x));
+  }
+  return __builtin_amdgcn_readfirstlane(s);
+}
+
+// The rows that a block of columns sees, as a list of tiles: those of the
+// first rows, then those of the windows.
+struct Sight {
+  int first, last;  // rows of its first and last token (last = -1: it sees none)
+  int head_tiles;   // tiles that hold the first rows
+  int gap;          // added to later tile numbers
+  int tiles;
+  __device__ __forceinline__ Sight(const PagedParams& p, const Sequence& sq, int x0, int cols, int tile_rows) {
+    first = max(sq.row0 + p.fgroup.div(x0), 0);
+    last = max(min(sq.row0 + p.fgroup.div(x0 + cols - 1), sq.most - 1), -1);
+    const int lo = max(first - p.window + 1, 0), n = last + 1;
+    head_tiles = (min(p.sinks, lo) + tile_rows - 1) / tile_rows;
+    gap = max(lo / tile_rows - head_tiles, 0);
+    tiles = max((n + tile_rows - 1) / tile_rows - gap, 0);
+  }
+  __device__ __forceinline__ int tile(int i) const { return i < head_tiles ? i : i + gap; }
+  __device__ __forceinline__ int per_slice(const PagedParams& p) const {
+    const int even = (tiles + p.slices - 1) / p.slices;
+    return even > p.min_tiles ? even : p.min_tiles;
+  }
+};
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <typename T, int D>
+struct Tile;
+
+// bf16: tiles of two blocks, one k step of the value product.
+template <int D>
+struct Tile<bf16, D> {
+  static constexpr int NB = 2, KS = D / 32, VE = D / 16, JJ = 1, NO = VE;
+  u32x4 k[NB][KS];
+  uint32_t v[NB][4][VE / 2];
+  __device__ __forceinline__ void load_k(int b, const bf16* row, int g) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) k[b][s] = ld16(row + (4 * s + g) * 8);
+  }
+  __device__ __forceinline__ void load_v(int b, int r, const bf16* row, int m) {
+    if constexpr (VE == 8) {
+      const u32x4 t = ld16(row + VE * m);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[b][r][i] = t[i];
+    } else {
+      const u32x2 t = *reinterpret_cast<const u32x2*>(row + VE * m);
+      v[b][r][0] = t[0];
+      v[b][r][1] = t[1];
+    }
+  }
+  __device__ __forceinline__ void zero_v(int b, int r) {
+#pragma unroll
+    for (int i = 0; i < VE / 2; ++i) v[b][r][i] = 0;
+  }
+  struct Query {
+    bf16x8 f[KS];
+    __device__ __forceinline__ void load(const bf16* row, int g, bool on) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        u32x4 t = {0u, 0u, 0u, 0u};
+        if (on) t = ld16(row + (4 * s + g) * 8);
+        f[s] = __builtin_bit_cast(bf16x8, t);
+      }
+    }
+  };
+  __device__ __forceinline__ f32x4 scores(int b, const Query& q) const {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[b][i]), q.f[i], s, 0, 0, 0);
+    return s;
+  }
+  // The probabilities enter as two bf16 terms, p = hi + lo: one would round
+  // each to 2^-9 of itself, two keep 2^-17, and the second product is hidden
+  // behind the loads.
+  __device__ __forceinline__ void values(const float* p, f32x4* o) const {
+    bf16x8 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      hi[i] = (bf16)p[i];
+      lo[i] = (bf16)(p[i] - (float)hi[i]);
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      u32x4 a;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; r += 2)
+          a[2 * b + r / 2] =
+              __builtin_amdgcn_perm(v[b][r + 1][e / 2], v[b][r][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+      const bf16x8 f = __builtin_bit_cast(bf16x8, a);
+      o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi, o[e], 0, 0, 0);
+      o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo, o[e], 0, 0, 0);
+    }
+  }
+};
+
+// fp32: four rows per k step. Tiles of one block at D = 128 keep two tiles in
+// the registers.
+template <int D>
+struct Tile<float, D> {
+  static constexpr int NB = D == 64 ? 2 : 1, KS = D / 16, VE = 4, JJ = D / 64, NO = 4 * JJ;
+  f32x4 k[NB][KS];
+  f32x4 v[NB][4][JJ];
+  __device__ __forceinline__ void load_k(int b, const float* row, int g) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) k[b][s] = *reinterpret_cast<const f32x4*>(row + 16 * s + 4 * g);
+  }
+  __device__ __forceinline__ void load_v(int b, int r, const float* row, int m) {
+#pragma unroll
+    for (int j = 0; j < JJ; ++j) v[b][r][j] = *reinterpret_cast<const f32x4*>(row + 64 * j + 4 * m);
+  }
+  __device__ __forceinline__ void zero_v(int b, int r) {
+#pragma unroll
+    for (int j = 0; j < JJ; ++j) v[b][r][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  struct Query {
+    f32x4 f[KS];
+    __device__ __forceinline__ void load(const float* row, int g, bool on) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        f[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (on) f[s] = *reinterpret_cast<const f32x4*>(row + 16 * s + 4 * g);
+      }
+    }
+  };
+  __device__ __forceinline__ f32x4 scores(int b, const Query& q) const {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b][i][e], q.f[i][e], s, 0, 0, 0);
+    return s;
+  }
+  __device__ __forceinline__ void values(const float* p, f32x4* o) const {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < JJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][r][j][e], p[4 * b + r], o[4 * j + e], 0, 0, 0);
+  }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(PagedParams p) {
+  typedef Tile<T, D> Tl;
+  constexpr int NB = Tl::NB, TR = NB * kBlock;
+  __shared__ float so[kWaves][kCols][D];
+  __shared__ float sm[kWaves][kCols], sl[kWaves][kCols];
+
+  // slices fastest, then K/V heads, then blocks of columns
+  int id = (int)blockIdx.x;
+  int up = p.fslices.div(id);
+  const int slice = id - up * p.slices;
+  const int blk = p.fhk.div(up), hk = up - blk * p.hk;
+  const int s = find_sequence(p.batch, [&](int c) { return first_block(p, c); }, blk);
+  Sequence sq;
+  sq.set(p, s);
+  const int x0 = (blk - first_block(p, s)) * kCols;
+  if (sq.seq < 0 || x0 < 0 || x0 >= sq.cols) return;
+  const int cols = min(sq.cols - x0, kCols);
+  const Sight sight(p, sq, x0, cols, TR);
+  const int per = sight.per_slice(p);
+  const int first = slice * per, last = min(first + per, sight.tiles);
+  if (first >= last && p.slices > 1) return;  // no rows: the join does not read this slice
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int m = lane % 16, g = lane / 16;
+
+  // the lane's column: its query, and the rows lo < j <= row that it sees
+  const int mx0 = x0 + (m < cols ? m : 0), tok = p.fgroup.div(mx0);
+  const int row = m < cols ? max(sq.row0 + tok, -1) : -1, lo = row - p.window;
+  typename Tl::Query q;
+  q.load(reinterpret_cast<const T*>(p.q) + (sq.t0 + tok) * p.q_ts + (int64_t)(hk * p.group + mx0 - tok * p.group) * p.q_hs,
+         g, m < cols);
+
+  const int32_t* table = p.table + (int64_t)s * p.max_pages;
+  const int64_t page_rows = (int64_t)p.hk * p.page_size;
+  const T* kp = reinterpret_cast<const T*>(p.k);
+  const T* vp = reinterpret_cast<const T*>(p.v);
+
+  // Page number and first slot of a block; -1 where the sequence or the table
+  // has none (its rows are then not seen).
+  auto page_of = [&](int blk, int* slot) {
+    *slot = 0;
+    if (blk * kBlock > sight.last) return -1;
+    const int pg = p.page_blocks.div(blk);
+    *slot = (blk - pg * p.page_blocks.d) * kBlock;
+    const int at = __builtin_amdgcn_readfirstlane(table[pg]);
+    return at >= 0 && at < p.n_pages ? at : -1;
+  };
+
+  f32x4 o[Tl::NO];
+#pragma unroll
+  for (int i = 0; i < Tl::NO; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float mx = -INFINITY, sum = 0.0f;
+
+  struct Place {
+    int page[NB], slot[NB];
+  };
+  auto place = [&](int i) {
+    Place w;
+    const int t = sight.tile(min(i, last - 1));
+#pragma unroll
+    for (int b = 0; b < NB; ++b) w.page[b] = page_of(t * NB + b, &w.slot[b]);
+    return w;
+  };
+  auto fetch = [&](const Place& w, Tl& t) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      // a block without a page reads page 0 instead, whose rows exist
+      const int64_t at = w.page[b] < 0 ? 0 : w.page[b] * page_rows + (int64_t)hk * p.page_size + w.slot[b];
+      const T* kb = kp + at * D;
+      const T* vb = vp + at * D;
+      t.load_k(b, kb + m * D, g);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) t.load_v(b, r, vb + (4 * g + r) * D, m);
+    }
+  };
+  auto use = [&](int i, const Place& w, Tl& t) {
+    const int row0 = sight.tile(i) * TR;
+    f32x4 sc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sc[b] = t.scores(b, q);
+    float pr[4 * NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) pr[4 * b + r] = sc[b][r] * p.scale_log2;
+    bool whole = row0 + TR - 1 <= sight.first && (row0 > sight.last - p.window || row0 + TR <= p.sinks);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) whole = whole && w.page[b] >= 0;
+    if (!whole) {
+      // what is not seen counts for nothing, whatever its bits are
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = row0 + b * kBlock + 4 * g + r;
+          if (w.page[b] < 0 || j > row || (j <= lo && j >= p.sinks)) pr[4 * b + r] = -INFINITY;
+          if (w.page[b] < 0 || j > sight.last || (j <= sight.first - p.window && j >= p.sinks)) t.zero_v(b, r);
+        }
+    }
+    float top = pr[0];
+#pragma unroll
+    for (int r = 1; r < 4 * NB; ++r) top = fmaxf(top, pr[r]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float now = fmaxf(mx, top);
+    const float ref = now == -INFINITY ? 0.0f : now;
+    const float back = fast_exp2(mx - ref);
+    mx = now;
+    float add = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 4 * NB; ++r) {
+      pr[r] = fast_exp2(pr[r] - ref);
+      add += pr[r];
+    }
+    sum = sum * back + add;
+#pragma unroll
+    for (int k = 0; k < Tl::NO; ++k) o[k] *= back;
+    t.values(pr, o);
+  };
+
+  // The next tile is on its way while this one is multiplied, and its page
+  // numbers came a tile before that. Past the slice's end its last tile is
+  // fetched again (a cache hit): with a load under a condition the compiler
+  // would have to wait for every load at the next use.
+  int i = first + wave;
+  if (i < last) {
+    Tl ta, tb;
+    Place wa = place(i), wb = place(i + kWaves);
+    fetch(wa, ta);
+    while (true) {
+      fetch(wb, tb);
+      const Place wn = place(i + 2 * kWaves);
+      use(i, wa, ta);
+      i += kWaves;
+      if (i >= last) break;
+      fetch(wn, ta);
+      const Place wm = place(i + 2 * kWaves);
+      use(i, wb, tb);
+      i += kWaves;
+      if (i >= last) break;
+      wa = wn;
+      wb = wm;
+    }
+  }
+
+  // join the four waves
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (g == 0) {
+    sm[wave][m] = mx;
+    sl[wave][m] = sum;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int j = 0; j < Tl::JJ; ++j)
+#pragma unroll
+      for (int e = 0; e < Tl::VE; ++e) so[wave][m][64 * j + Tl::VE * (4 * g + r) + e] = o[j * Tl::VE + e][r];
+  __syncthreads();
+  constexpr int C4 = D / 4;
+  for (int at = threadIdx.x; at < cols * C4; at += kThreads) {
+    const int h = at / C4, c = (at % C4) * 4;
+    float top = sm[0][h];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sm[w][h]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float l = 0.0f;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = fast_exp2(sm[w][h] - ref);
+      l += f * sl[w][h];
+      acc += f * *reinterpret_cast<const f32x4*>(&so[w][h][c]);
+    }
+    const int tk = p.fgroup.div(x0 + h);
+    const int64_t orow = (int64_t)(sq.t0 + tk) * p.hq + hk * p.group + (x0 + h - tk * p.group);
+    if (p.slices == 1) {
+      const float inv = l > 0.0f ? 1.0f / l : l;  // nothing seen: zero (and a NaN stays one)
+      float res[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+      store4(reinterpret_cast<T*>(p.out) + orow * D + c, res);
+      if (p.lse && c == 0) p.lse[orow] = (top + __log2f(l)) * 0.69314718055994530942f;
+    } else {
+      *reinterpret_cast<f32x4*>(p.part_o + (orow * p.slices + slice) * D + c) = acc;
+      if (c == 0) p.part_ml[orow * p.slices + slice] = make_float2(top, l);
+    }
+  }
+}
+
+// Joins the slices of a (token, head) in a fixed order: a lane per four
+// channels, the streams of slices joined through LDS.
+template <typename T, int D, int TR>
+__global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
+  constexpr int C4 = D / 4, NS = kThreads / C4;
+  __shared__ float so[NS][D];
+  __shared__ float sl[NS];
+  const int row = blockIdx.x, tok = row / p.hq, head = (row - tok * p.hq) % p.group;
+  const int s0 = p.cu ? find_sequence(p.batch, [&](int c) { return p.cu[c]; }, tok) : tok;
+  Sequence sq;
+  sq.set(p, s0);
+  const int x = (tok - sq.t0) * p.group + head;
+  if (sq.seq < 0 || x < 0 || x >= sq.cols) return;  // behind the last sequence
+  const int x0 = p.cu ? x / kCols * kCols : head / kCols * kCols;
+  const Sight sight(p, sq, x0, min(sq.cols - x0, kCols), TR);
+  const int per = sight.per_slice(p);
+  const int live = (sight.tiles + per - 1) / per;
+  const float2* ml = p.part_ml + (int64_t)row * p.slices;
+  const float* po = p.part_o + (int64_t)row * p.slices * D;
+  float top = -INFINITY;
+  for (int s = threadIdx.x % kWave; s < live; s += kWave) top = fmaxf(top, ml[s].x);
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  const int c = (threadIdx.x % C4) * 4, st = threadIdx.x / C4;
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  float l = 0.0f;
+  for (int s = st; s < live; s += NS) {
+    const float2 x = ml[s];
+    const float f = fast_exp2(x.x - ref);
+    l += f * x.y;
+    acc += f * *reinterpret_cast<const f32x4*>(po + (int64_t)s * D + c);
+  }
+  *reinterpret_cast<f32x4*>(&so[st][c]) = acc;
+  if (c == 0) sl[st] = l;
+  __syncthreads();
+  if (st == 0) {
+    l = 0.0f;
+    acc = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      l += sl[s];
+      acc += *reinterpret_cast<const f32x4*>(&so[s][c]);
+    }
+    const float inv = l > 0.0f ? 1.0f / l : l;
+    float res[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+    store4(reinterpret_cast<T*>(p.out) + (int64_t)row * D + c, res);
+    if (p.lse && c == 0) p.lse[row] = (top + __log2f(l)) * 0.69314718055994530942f;
+  }
+}
+
+// Blocks of columns of a call (n_tokens < 0: one token of every sequence).
+int64_t col_blocks(int group, int64_t n_tokens, int batch) {
+  return n_tokens < 0 ? (int64_t)batch * ((group + kCols - 1) / kCols) : n_tokens * group / kCols + batch;
+}
+
+int tile_rows(const HeadsDims& d) { return kBlock * (d.esize == 4 && d.d == 128 ? 1 : 2); }
+
+template <typename T, int D>
+hipError_t attention_on(const PagedParams& p, hipStream_t s) {
+  const bool tr = trace_on();
+  const unsigned groups = (unsigned)((int64_t)col_blocks(p.group, p.cu ? p.n_tokens : -1, p.batch) * p.hk * p.slices);
+  if (tr) trace_begin("paged_attention", s);
+  paged_attention_kernel<T, D><<<dim3(groups), kThreads, 0, s>>>(p);
+  hipError_t e = hipGetLastError();
+  if (tr) trace_end(s);
+  if (e != hipSuccess || p.slices == 1) return e;
+  if (tr) trace_begin("paged_join", s);
+  paged_join_kernel<T, D, Tile<T, D>::NB * kBlock><<<dim3((unsigned)(p.n_tokens * p.hq)), kThreads, 0, s>>>(p);
+  e = hipGetLastError();
+  if (tr) trace_end(s);
+  return e;
+}
+
+}  // namespace
+
+PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragged, int64_t max_kv_len, int64_t window,
+                     int64_t sinks) {
+  // Enough workgroups to keep every CU's loads in flight, slices of no less
+  // than a tile per wave.
+  const int tr = tile_rows(d);
+  window = std::min<int64_t>(window, INT32_MAX);
+  sinks = std::min<int64_t>(sinks, INT32_MAX);
+  int64_t rows = std::min<int64_t>(max_kv_len, INT32_MAX);
+  if (window > 0 && rows > window + sinks + 2 * tr) rows = window + sinks + 2 * tr;
+  const int64_t tiles = std::max<int64_t>(1, (rows + tr - 1) / tr);
+  PagedPlan pl;
+  pl.min_tiles = kWaves;
+  pl.groups = col_blocks(d.hq / d.hk, ragged ? n_tokens : -1, batch) * d.hk;
+  int64_t s = std::min<int64_t>((2048 + pl.groups - 1) / pl.groups, (tiles + pl.min_tiles - 1) / pl.min_tiles);
+  s = std::max<int64_t>(1, std::min<int64_t>(s, kMaxSlices));
+  pl.slices = (int)s;
+  pl.bytes = s == 1 ? 0 : (size_t)n_tokens * d.hq * s * (d.d * sizeof(float) + sizeof(float2));
+  pl.bytes = (pl.bytes + 255) / 256 * 256;
+  return pl;
+}
+
+hipError_t launch_paged_attention(const HeadsDims& d, const PagedDims& c, const PagedPlan& pl, int64_t n_tokens,
+                                  const int32_t* cu_tokens, const Rows& q, float scale, int64_t window, int64_t sinks,
+                                  void* out, float* lse, char* ws, hipStream_t s) {
+  PagedParams p{};
+  p.q = q.p;
+  p.q_ts = q.ts;
+  p.q_hs = q.hs;
+  p.k = c.k;
+  p.v = c.v;
+  p.table = c.table;
+  p.kv_len = c.kv_len;
+  p.cu = cu_tokens;
+  p.n_pages = c.n_pages;
+  p.page_size = c.page_size;
+  p.max_pages = c.max_pages;
+  p.batch = c.batch;
+  p.n_tokens = (int)n_tokens;
+  p.page_blocks = FastDiv(c.page_size / kBlock);
+  p.hq = d.hq;
+  p.hk = d.hk;
+  p.group = d.hq / d.hk;
+  p.slices = pl.slices;
+  p.min_tiles = pl.min_tiles;
+  p.fslices = FastDiv(pl.slices);
+  p.fhk = FastDiv(d.hk);
+  p.fgroup = FastDiv(p.group);
+  p.window = window > 0 ? (int)std::min<int64_t>(window, INT32_MAX) : INT32_MAX;
+  p.sinks = (int)std::min<int64_t>(sinks, INT32_MAX);
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.out = out;
+  p.lse = lse;
+  p.part_o = reinterpret_cast<float*>(ws);
+  p.part_ml = reinterpret_cast<float2*>(ws + (size_t)n_tokens * d.hq * pl.slices * d.d * sizeof(float));
+  if (d.esize == 2) return d.d == 64 ? attention_on<bf16, 64>(p, s) : attention_on<bf16, 128>(p, s);
+  return d.d == 64 ? attention_on<float, 64>(p, s) : attention_on<float, 128>(p, s);
+}
+
+}  // namespace pf

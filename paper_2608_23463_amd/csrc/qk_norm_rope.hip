@@ -1,0 +1,596 @@
+// Queries and keys normed per head and turned by their positions: in training
+// (forward, backward) and on the way into a paged cache (append).
+//
+//   z = x * rstd * gamma,  rstd = (mean(x^2) + eps)^-1/2   (without norm z = x)
+//   pair (a, b) of the first rot elements, angle t = position * frequency:
+//   y_a = z_a cos t - z_b sin t,  y_b = z_a sin t + z_b cos t
+//
+// A wave takes TPW consecutive tokens. It forms their cosines and sines once,
+// one pair per lane, and keeps them in LDS for all heads of the tokens. Then
+// the (token, head) rows of a tensor run through the wave in passes: D / 16
+// lanes hold a row, 16 elements each, both members of eight pairs, so the
+// rotation needs no exchange and the norm one sum over those lanes.
+// Bound by HBM: every row is read and written once, in 16-byte accesses.
+#include "heads.hpp"
+#include "trace.hpp"
+
+namespace pf {
+
+int heads_dims(const pf_heads_config* c, HeadsDims* d, const char** why) {
+  *why = "";
+  if (!c) {
+    *why = "config is NULL";
+    return PF_ERR_INVALID_ARG;
+  }
+  if (c->dtype != PF_BF16 && c->dtype != PF_FP32) {
+    *why = "dtype must be PF_BF16 or PF_FP32";
+    return PF_ERR_INVALID_ARG;
+  }
+  if (c->n_heads < 1 || c->n_kv_heads < 1 || c->n_heads % c->n_kv_heads != 0) {
+    *why = "n_heads must be a positive multiple of n_kv_heads";
+    return PF_ERR_INVALID_ARG;
+  }
+  if (c->n_heads > 4096) {
+    *why = "more than 4096 heads";
+    return PF_ERR_UNSUPPORTED;
+  }
+  if (c->head_dim != 64 && c->head_dim != 128) {
+    *why = "head_dim must be 64 or 128";
+    return PF_ERR_UNSUPPORTED;
+  }
+  if (c->norm != PF_NORM_NONE && c->norm != PF_NORM_RMS) {
+    *why = "norm must be PF_NORM_NONE or PF_NORM_RMS";
+    return PF_ERR_INVALID_ARG;
+  }
+  if (c->norm == PF_NORM_RMS && !(c->eps >= 0.0f && c->eps < 1e30f)) {
+    *why = "eps must be finite and not negative";
+    return PF_ERR_INVALID_ARG;
+  }
+  if (c->rot_dim < 0 || c->rot_dim > c->head_dim || c->rot_dim % 16 != 0) {
+    *why = "rot_dim must be a multiple of 16 in 0..head_dim";
+    return PF_ERR_INVALID_ARG;
+  }
+  if (c->rope_style != PF_ROPE_HALVES && c->rope_style != PF_ROPE_PAIRS) {
+    *why = "rope_style must be PF_ROPE_HALVES or PF_ROPE_PAIRS";
+    return PF_ERR_INVALID_ARG;
+  }
+  if (c->n_axes < 1 || c->n_axes > PF_MAX_AXES) {
+    *why = "n_axes must be in 1..PF_MAX_AXES";
+    return PF_ERR_INVALID_ARG;
+  }
+  int end = 0;
+  for (int i = 0; i < PF_MAX_AXES; ++i) {
+    if (i < c->n_axes) {
+      if (c->axis_pairs[i] < 0 || c->axis_pairs[i] > c->rot_dim / 2) {
+        *why = "axis_pairs must not be negative or above rot_dim / 2";
+        return PF_ERR_INVALID_ARG;
+      }
+      end += c->axis_pairs[i];
+    }
+    d->axis_end[i] = end;
+  }
+  if (end != c->rot_dim / 2) {
+    *why = "axis_pairs must add up to rot_dim / 2";
+    return PF_ERR_INVALID_ARG;
+  }
+  d->hq = c->n_heads;
+  d->hk = c->n_kv_heads;
+  d->d = c->head_dim;
+  d->esize = c->dtype == PF_BF16 ? 2 : 4;
+  d->norm = c->norm;
+  d->eps = c->eps;
+  d->rot = c->rot_dim;
+  d->pairs_style = c->rope_style == PF_ROPE_PAIRS;
+  d->n_axes = c->n_axes;
+  return PF_OK;
+}
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+
+struct TurnParams {
+  const double* freqs;
+  const int32_t* positions;  // [n_axes, n] or NULL (append: by the cache)
+  int64_t n;
+  int rot, n_axes;
+  int axis_end[PF_MAX_AXES];
+};
+
+// Rotation and norm of one launch.
+struct QkParams {
+  TurnParams turn;
+  Rows q, k, v, q_out, k_out;
+  const void* gamma_q;
+  const void* gamma_k;
+  int hq, hk;
+  FastDiv fq, fk;
+  float eps;
+  int norm;
+  int parts;  // waves that share a token block's passes
+  FastDiv fparts;
+  // append
+  char* k_pages;
+  char* v_pages;
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* cu;
+  int n_pages, page_size, max_pages, batch;
+  FastDiv fpage;
+};
+
+// Cosine and sine of position * frequency. Far positions need more than 32
+// bits: a position of 2^20 in fp32 leaves an angle off by up to 2^-4. The
+// angle is formed in revolutions in 64 bits and its whole revolutions dropped
+// there, so what fp32 sees is below half a revolution and off by at most 2^-26.
+__device__ __forceinline__ float2 turn_of(double freq, int pos) {
+  const double rev = (double)pos * freq * 0.15915494309189533577;
+  const float f = (float)(rev - rint(rev));
+  float2 cs;
+  sincospif(2.0f * f, &cs.y, &cs.x);
+  return cs;
+}
+
+__device__ __forceinline__ int axis_of(const TurnParams& t, int pair) {
+  int a = 0;
+#pragma unroll
+  for (int i = 0; i < PF_MAX_AXES - 1; ++i) a += pair >= t.axis_end[i];
+  return a;
+}
+
+// Where a lane's 16 elements of a row sit. Chunk c of D / 16; `turned` tells
+// whether its pairs are among the rotated ones.
+//  halves: members of pair p at p and rot / 2 + p. The elements past rot are
+//  split in halves the same way, so every chunk is two runs of eight.
+//  pairs: members at 2p and 2p + 1, one run of sixteen.
+template <int D, bool PAIRS>
+struct Chunk {
+  int a, b;
+  bool turned;
+  __device__ __forceinline__ Chunk(int c, int rot) {
+    if (PAIRS) {
+      a = 16 * c;
+      b = a + 8;
+      turned = a < rot;
+    } else {
+      turned = 16 * c < rot;
+      const int e = turned ? 8 * c : 8 * c - rot / 2;
+      a = turned ? e : rot + e;
+      b = turned ? rot / 2 + e : rot + (D - rot) / 2 + e;
+    }
+  }
+};
+
+// Member registers of pair i of a lane: v[ia(i)], v[ib(i)].
+template <bool PAIRS>
+__device__ __forceinline__ constexpr int ia(int i) { return PAIRS ? 2 * i : i; }
+template <bool PAIRS>
+__device__ __forceinline__ constexpr int ib(int i) { return PAIRS ? 2 * i + 1 : 8 + i; }
+
+template <bool PAIRS>
+__device__ __forceinline__ void rotate(float* v, const float2* cs, bool turned, float sign) {
+  if (!turned) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = v[ia<PAIRS>(i)], b = v[ib<PAIRS>(i)], c = cs[i].x, s = sign * cs[i].y;
+    v[ia<PAIRS>(i)] = a * c - b * s;
+    v[ib<PAIRS>(i)] = a * s + b * c;
+  }
+}
+
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v) {
+#pragma unroll
+  for (int o = 1; o < LPR; o <<= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void load16(const T* p, int a, int b, Raw8<T>* r) {
+  raw_load8(p + a, r[0]);
+  raw_load8(p + b, r[1]);
+}
+
+// Position of token t of the launch on an axis.
+__device__ __forceinline__ int position_of(const TurnParams& t, int64_t tok, int axis) {
+  return t.positions[(int64_t)axis * t.n + tok];
+}
+
+// Sequence of a token of a ragged batch: the number of boundaries cu[1..B]
+// at or before it, counted by the wave, 64 at a time. B: behind the last one.
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int64_t tok) {
+  int s = 0;
+  for (int i = 0; i < batch; i += kWave) {
+    const int at = i + (int)(threadIdx.x & (kWave - 1));
+    s += __popcll(__ballot(at < batch && cu[at + 1] <= tok));
+  }
+  return s;
+}
+
+// KIND 0: forward into tensors; 1: append into pages.
+template <typename T, int D, bool PAIRS, int TPW, int KIND>
+__global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p) {
+  constexpr int LPR = D / 16, RPP = kWave / LPR;  // lanes per row, rows per pass
+  __shared__ float2 turns[kWaves][TPW][D / 2];
+  __shared__ int64_t rows[kWaves][TPW];  // append: row (head 0) of each token in a page, or -1
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int unit = (int)(blockIdx.x * kWaves + wave), block = p.fparts.div(unit);
+  const int64_t t0 = (int64_t)block * TPW;
+  const int part = unit - block * p.parts;
+  const int tokens = (int)min((int64_t)TPW, p.turn.n - t0);
+  if (tokens <= 0) return;  // waves share nothing: no barrier below
+  const int row = lane / LPR;
+  const Chunk<D, PAIRS> ch(lane % LPR, p.turn.rot);
+
+  for (int i = 0; i < tokens; ++i) {
+    int at = 0;
+    if (KIND == 1) {
+      // where the token goes: row kv_len - new + i of its sequence
+      const int64_t tok = t0 + i;
+      const int s = p.cu ? sequence_of(p.cu, p.batch, tok) : (int)tok;
+      int64_t dst = -1;  // behind the last sequence, or without a place: left alone
+      if (s < p.batch) {
+        const int64_t pos = p.cu ? (int64_t)p.kv_len[s] - p.cu[s + 1] + tok : (int64_t)p.kv_len[s] - 1;
+        at = (int)pos;
+        if (pos >= 0 && pos < (int64_t)p.max_pages * p.page_size) {
+          const int pg = p.fpage.div((int)pos);
+          const int id = p.table[(int64_t)s * p.max_pages + pg];
+          if (id >= 0 && id < p.n_pages) dst = (int64_t)id * p.hk * p.page_size + ((int)pos - pg * p.page_size);
+        }
+      }
+      if (lane == 0) rows[wave][i] = dst;
+    }
+    for (int pair = lane; pair < D / 2; pair += kWave) {
+      float2 cs = make_float2(1.0f, 0.0f);
+      if (pair < p.turn.rot / 2) {
+        if (KIND == 0 || p.turn.positions) at = position_of(p.turn, t0 + i, axis_of(p.turn, pair));
+        cs = turn_of(p.turn.freqs[pair], at);
+      }
+      turns[wave][i][pair] = cs;
+    }
+  }
+  __builtin_amdgcn_wave_barrier();  // LDS of the wave's own: in order without a workgroup barrier
+
+  auto run = [&](const Rows& in, const Rows& out, const void* gamma, int heads, const FastDiv& fd, int which) {
+    const int items = tokens * heads;
+    float g[16];
+    if (p.norm && which < 2) {
+      if (gamma) {
+        load8(static_cast<const T*>(gamma) + ch.a, g);
+        load8(static_cast<const T*>(gamma) + ch.b, g + 8);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) g[i] = 1.0f;
+      }
+    }
+    for (int base = part * RPP; base < items; base += p.parts * RPP) {
+      const int it = base + row;
+      const bool on = it < items;
+      const int tk = on ? fd.div(it) : 0, h = on ? it - tk * heads : 0;
+      const T* src = reinterpret_cast<const T*>(in.p) + (t0 + tk) * in.ts + h * in.hs;
+      float v[16];
+      Raw8<T> r[2];
+      load16(src, ch.a, ch.b, r);
+      raw_to_f32(r[0], v);
+      raw_to_f32(r[1], v + 8);
+      if (which < 2) {
+        if (p.norm) {
+          float ss = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) ss += v[i] * v[i];
+          const float rstd = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + p.eps);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] *= rstd * g[i];
+        }
+        rotate<PAIRS>(v, &turns[wave][tk][8 * (lane % LPR)], ch.turned, 1.0f);
+      }
+      T* dst;
+      bool write = on;
+      if (KIND == 1) {
+        const int64_t r0 = rows[wave][tk];
+        write = write && r0 >= 0;
+        dst = which == 0 ? reinterpret_cast<T*>(out.p) + (t0 + tk) * out.ts + h * out.hs
+                         : reinterpret_cast<T*>(which == 1 ? p.k_pages : p.v_pages) + (r0 + (int64_t)h * p.page_size) * D;
+      } else {
+        dst = reinterpret_cast<T*>(out.p) + (t0 + tk) * out.ts + h * out.hs;
+      }
+      if (write) {
+        store8(dst + ch.a, v);
+        store8(dst + ch.b, v + 8);
+      }
+    }
+  };
+  if (p.q.p) run(p.q, p.q_out, p.gamma_q, p.hq, p.fq, 0);
+  run(p.k, p.k_out, p.gamma_k, p.hk, p.fk, 1);
+  if (KIND == 1) run(p.v, p.v, nullptr, p.hk, p.fk, 2);
+}
+
+struct QkBwdParams {
+  TurnParams turn;
+  Rows q, k, dqo, dko, dq, dk;
+  const void* gamma_q;
+  const void* gamma_k;
+  int hq, hk;
+  FastDiv fq, fk;
+  float eps;
+  int norm;
+  float* part;  // [2][blocks][D]: gains' gradients of every workgroup
+};
+
+// dz = R(-t) dy; dgamma += dz * xn with xn = x rstd; g = dz gamma;
+// dx = rstd (g - xn mean(g xn)). A lane keeps the gains' gradients of its 16
+// elements over all its rows; the workgroups' sums are joined in a fixed order.
+template <typename T, int D, bool PAIRS, int TPW>
+__global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkBwdParams p) {
+  constexpr int LPR = D / 16, RPP = kWave / LPR;
+  __shared__ float2 turns[kWaves][TPW][D / 2];
+  __shared__ float sums[kWaves][D];
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int row = lane / LPR;
+  const Chunk<D, PAIRS> ch(lane % LPR, p.turn.rot);
+  float acc[2][16] = {};
+  const int64_t step = (int64_t)gridDim.x * kWaves * TPW;
+  for (int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * TPW; t0 < p.turn.n; t0 += step) {
+    const int tokens = (int)min((int64_t)TPW, p.turn.n - t0);
+    __builtin_amdgcn_wave_barrier();
+    for (int i = 0; i < tokens; ++i)
+      for (int pair = lane; pair < D / 2; pair += kWave) {
+        float2 cs = make_float2(1.0f, 0.0f);
+        if (pair < p.turn.rot / 2)
+          cs = turn_of(p.turn.freqs[pair], position_of(p.turn, t0 + i, axis_of(p.turn, pair)));
+        turns[wave][i][pair] = cs;
+      }
+    __builtin_amdgcn_wave_barrier();
+    auto run = [&](const Rows& x, const Rows& dy, const Rows& dx, const void* gamma, int heads, const FastDiv& fd,
+                   float* ac) {
+      const int items = tokens * heads;
+      float g[16];
+      if (p.norm) {
+        if (gamma) {
+          load8(static_cast<const T*>(gamma) + ch.a, g);
+          load8(static_cast<const T*>(gamma) + ch.b, g + 8);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) g[i] = 1.0f;
+        }
+      }
+      for (int base = 0; base < items; base += RPP) {
+        const int it = base + row;
+        const bool on = it < items;
+        const int tk = on ? fd.div(it) : 0, h = on ? it - tk * heads : 0;
+        float dz[16];
+        Raw8<T> r[2], rx[2];
+        load16(reinterpret_cast<const T*>(dy.p) + (t0 + tk) * dy.ts + h * dy.hs, ch.a, ch.b, r);
+        if (p.norm) load16(reinterpret_cast<const T*>(x.p) + (t0 + tk) * x.ts + h * x.hs, ch.a, ch.b, rx);
+        raw_to_f32(r[0], dz);
+        raw_to_f32(r[1], dz + 8);
+        rotate<PAIRS>(dz, &turns[wave][tk][8 * (lane % LPR)], ch.turned, -1.0f);
+        if (p.norm) {
+          float xn[16];
+          raw_to_f32(rx[0], xn);
+          raw_to_f32(rx[1], xn + 8);
+          float ss = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) ss += xn[i] * xn[i];
+          const float rstd = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + p.eps);
+          float dot = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            xn[i] *= rstd;
+            if (on) ac[i] += dz[i] * xn[i];
+            dz[i] *= g[i];
+            dot += dz[i] * xn[i];
+          }
+          const float mean = row_sum<LPR>(dot) * (1.0f / D);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) dz[i] = rstd * (dz[i] - xn[i] * mean);
+        }
+        if (on) {
+          T* dst = reinterpret_cast<T*>(dx.p) + (t0 + tk) * dx.ts + h * dx.hs;
+          store8(dst + ch.a, dz);
+          store8(dst + ch.b, dz + 8);
+        }
+      }
+    };
+    run(p.q, p.dqo, p.dq, p.gamma_q, p.hq, p.fq, acc[0]);
+    run(p.k, p.dko, p.dk, p.gamma_k, p.hk, p.fk, acc[1]);
+  }
+  if (!p.norm || !p.part) return;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float v = acc[w][i];
+#pragma unroll
+      for (int o = LPR; o < kWave; o <<= 1) v += __shfl_xor(v, o);
+      if (row == 0) sums[wave][i < 8 ? ch.a + i : ch.b + i - 8] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x < D) {
+      float v = 0.0f;
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) v += sums[k][threadIdx.x];
+      p.part[((int64_t)w * gridDim.x + blockIdx.x) * D + threadIdx.x] = v;
+    }
+    __syncthreads();
+  }
+}
+
+// dgamma[w][c] = sum over the workgroups' rows, in a fixed order: 64 columns
+// per workgroup, 16 streams of rows joined through LDS.
+__global__ void __launch_bounds__(1024) qk_gain_kernel(const float* part, int blocks, int D, float* dgq, float* dgk) {
+  __shared__ float sums[16][64];
+  const int w = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 63), st = threadIdx.x >> 6;
+  float v = 0.0f;
+  for (int b = st; b < blocks; b += 16) v += part[((int64_t)w * blocks + b) * D + c];
+  sums[st][threadIdx.x & 63] = v;
+  __syncthreads();
+  if (st == 0) {
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += sums[i][threadIdx.x];
+    float* out = w ? dgk : dgq;
+    if (out) out[c] = v;
+  }
+}
+
+TurnParams turn_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, const int32_t* positions) {
+  TurnParams t;
+  t.freqs = w.freqs;
+  t.positions = positions;
+  t.n = n;
+  t.rot = d.rot;
+  t.n_axes = d.n_axes;
+  for (int i = 0; i < PF_MAX_AXES; ++i) t.axis_end[i] = d.axis_end[i];
+  return t;
+}
+
+constexpr int kTokensPerWave = 4;
+
+template <class F>
+hipError_t timed(const char* label, hipStream_t s, F&& f) {
+  const bool tr = trace_on();
+  if (tr) trace_begin(label, s);
+  f();
+  const hipError_t e = hipGetLastError();
+  if (tr) trace_end(s);
+  return e;
+}
+
+template <typename T, int D, bool PAIRS, int KIND>
+hipError_t forward_on(QkParams p, int64_t n, const char* label, hipStream_t s) {
+  // few tokens: one per wave and several waves to a token, so that a call of
+  // one token still spreads its heads; many: four per wave
+  const int rows = 64 / (D / 16);
+  const int passes = ((p.q.p && p.hq > p.hk ? p.hq : p.hk) + rows - 1) / rows;
+  return timed(label, s, [&] {
+    if (n < 2048) {
+      p.parts = passes;
+      p.fparts = FastDiv(p.parts);
+      const int64_t units = n * p.parts;
+      qk_forward_kernel<T, D, PAIRS, 1, KIND><<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
+    } else {
+      p.parts = 1;
+      const int64_t units = (n + kTokensPerWave - 1) / kTokensPerWave;
+      qk_forward_kernel<T, D, PAIRS, kTokensPerWave, KIND>
+          <<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
+    }
+  });
+}
+
+template <int KIND>
+hipError_t forward_any(const HeadsDims& d, const QkParams& p, int64_t n, const char* label, hipStream_t s) {
+  if (d.esize == 2) {
+    if (d.d == 64)
+      return d.pairs_style ? forward_on<bf16, 64, true, KIND>(p, n, label, s) : forward_on<bf16, 64, false, KIND>(p, n, label, s);
+    return d.pairs_style ? forward_on<bf16, 128, true, KIND>(p, n, label, s) : forward_on<bf16, 128, false, KIND>(p, n, label, s);
+  }
+  if (d.d == 64)
+    return d.pairs_style ? forward_on<float, 64, true, KIND>(p, n, label, s) : forward_on<float, 64, false, KIND>(p, n, label, s);
+  return d.pairs_style ? forward_on<float, 128, true, KIND>(p, n, label, s) : forward_on<float, 128, false, KIND>(p, n, label, s);
+}
+
+QkParams qk_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, const int32_t* positions) {
+  QkParams p{};
+  p.turn = turn_params(d, w, n, positions);
+  p.gamma_q = w.gamma_q;
+  p.gamma_k = w.gamma_k;
+  p.hq = d.hq;
+  p.hk = d.hk;
+  p.fq = FastDiv(d.hq);
+  p.fk = FastDiv(d.hk);
+  p.eps = d.eps;
+  p.norm = d.norm;
+  p.parts = 1;
+  return p;
+}
+
+constexpr int kBwdTokens = 4;      // tokens per wave and step of the backward
+constexpr int kBwdBlocks = 2048;   // workgroups at most (their gain sums are joined)
+
+int bwd_blocks(int64_t n) {
+  const int64_t per = (int64_t)kWaves * kBwdTokens;
+  const int64_t b = (n + per - 1) / per;
+  return (int)(b < kBwdBlocks ? b : kBwdBlocks);
+}
+
+template <typename T, int D, bool PAIRS>
+void backward_on(const QkBwdParams& p, int64_t n, hipStream_t s) {
+  qk_backward_kernel<T, D, PAIRS, kBwdTokens><<<dim3((unsigned)bwd_blocks(n)), kThreads, 0, s>>>(p);
+}
+
+}  // namespace
+
+hipError_t launch_qk_forward(const HeadsDims& d, const HeadsWeights& w, int64_t n, const Rows& q, const Rows& k,
+                             const int32_t* positions, const Rows& q_out, const Rows& k_out, hipStream_t s) {
+  QkParams p = qk_params(d, w, n, positions);
+  p.q = q;
+  p.k = k;
+  p.q_out = q_out;
+  p.k_out = k_out;
+  return forward_any<0>(d, p, n, "qk_norm_rope", s);
+}
+
+hipError_t launch_paged_append(const HeadsDims& d, const HeadsWeights& w, const PagedDims& c, int64_t n,
+                               const int32_t* cu_tokens, const Rows& q, const Rows& k, const Rows& v,
+                               const int32_t* positions, const Rows& q_out, hipStream_t s) {
+  QkParams p = qk_params(d, w, n, positions);
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.q_out = q_out;
+  p.k_pages = c.k;
+  p.v_pages = c.v;
+  p.table = c.table;
+  p.kv_len = c.kv_len;
+  p.cu = cu_tokens;
+  p.n_pages = c.n_pages;
+  p.page_size = c.page_size;
+  p.max_pages = c.max_pages;
+  p.batch = c.batch;
+  p.fpage = FastDiv(c.page_size);
+  return forward_any<1>(d, p, n, "paged_append", s);
+}
+
+size_t qk_backward_ws(const HeadsDims& d, int64_t n) {
+  return d.norm ? (size_t)2 * bwd_blocks(n) * d.d * sizeof(float) : 0;
+}
+
+hipError_t launch_qk_backward(const HeadsDims& d, const HeadsWeights& w, int64_t n, const Rows& q, const Rows& k,
+                              const int32_t* positions, const Rows& dq_out, const Rows& dk_out, const Rows& dq,
+                              const Rows& dk, float* dgamma_q, float* dgamma_k, float* ws, hipStream_t s) {
+  QkBwdParams p{};
+  p.turn = turn_params(d, w, n, positions);
+  p.q = q;
+  p.k = k;
+  p.dqo = dq_out;
+  p.dko = dk_out;
+  p.dq = dq;
+  p.dk = dk;
+  p.gamma_q = w.gamma_q;
+  p.gamma_k = w.gamma_k;
+  p.hq = d.hq;
+  p.hk = d.hk;
+  p.fq = FastDiv(d.hq);
+  p.fk = FastDiv(d.hk);
+  p.eps = d.eps;
+  p.norm = d.norm;
+  const bool gains = d.norm && (dgamma_q || dgamma_k);
+  p.part = gains ? ws : nullptr;
+  hipError_t e = n == 0 ? hipSuccess : timed("qk_backward", s, [&] {
+    if (d.esize == 2) {
+      if (d.d == 64) d.pairs_style ? backward_on<bf16, 64, true>(p, n, s) : backward_on<bf16, 64, false>(p, n, s);
+      else d.pairs_style ? backward_on<bf16, 128, true>(p, n, s) : backward_on<bf16, 128, false>(p, n, s);
+    } else {
+      if (d.d == 64) d.pairs_style ? backward_on<float, 64, true>(p, n, s) : backward_on<float, 64, false>(p, n, s);
+      else d.pairs_style ? backward_on<float, 128, true>(p, n, s) : backward_on<float, 128, false>(p, n, s);
+    }
+  });
+  if (e != hipSuccess || !gains) return e;
+  return timed("qk_gains", s, [&] {
+    qk_gain_kernel<<<dim3(d.d / 64, 2), 1024, 0, s>>>(ws, bwd_blocks(n), d.d, dgamma_q, dgamma_k);
+  });
+}
+
+}  // namespace pf
