@@ -34,6 +34,7 @@ FILE_FLAGS = {
     "attention_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "attention_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "decode_prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "paged_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

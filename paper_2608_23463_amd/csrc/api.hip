@@ -673,7 +673,7 @@ size_t proxy_paged_workspace_size(const pf_heads_config* cfg, int32_t batch, int
   if (heads_dims(cfg, &d, &why) != PF_OK || batch < 1 || n_tokens < 1 || n_tokens > INT32_MAX || max_new < 1 ||
       max_kv_len < 1 || window < 0 || sinks < 0)
     return 0;
-  return paged_plan(d, batch, n_tokens, ragged != 0, max_kv_len, window, sinks).bytes;
+  return paged_plan(d, batch, n_tokens, ragged != 0, max_new, max_kv_len, window, sinks).bytes;
 }
 
 int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cache, int64_t n_tokens,
@@ -703,7 +703,7 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
   const size_t out_bytes = (size_t)n * d.hq * d.d * d.esize;
   if (overlaps(out, out_bytes, q->p, rows_bytes(*q, n, d.hq, d)))
     return fail(PF_ERR_INVALID_ARG, "out must not overlap q");
-  const PagedPlan pl = paged_plan(d, c.batch, n, cu_tokens != nullptr, max_kv_len, window, sinks);
+  const PagedPlan pl = paged_plan(d, c.batch, n, cu_tokens != nullptr, max_new, max_kv_len, window, sinks);
   if (pl.groups > INT32_MAX / pl.slices) return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes");
   if (pl.bytes && (!workspace || ws_bytes < pl.bytes))
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", pl.bytes, workspace ? ws_bytes : 0);

@@ -17,6 +17,15 @@ __device__ __forceinline__ int lds_swz(int r, int c) {
   return C >= 16 ? c ^ (r & 15) : c ^ ((r / (16 / C)) & (C - 1));
 }
 
+// Chunk swizzle of a row-major value tile read through LDS transpose reads:
+// a read pass covers 4 consecutive rows (keys) at 4 consecutive chunks, so
+// the key moves rows by 64 bytes within each 256-byte bank window.
+template <int NC>
+__device__ __forceinline__ int vtr_swz(int r, int c) {
+  static_assert(NC == 8 || NC >= 16, "rows of 128 bytes or of 256 bytes and more");
+  return NC == 8 ? c ^ (((r >> 1) & 1) * 4) : c ^ ((r & 3) * 4);
+}
+
 // acc + 2^-8 A B^T for one 32x32 block of fp8 e5m2 operands over 64 K
 // elements: lane l supplies row l % 32 of A and of B, bytes
 // [32 (l / 32), +32) of the block's 64 (the same convention on both sides,

@@ -122,16 +122,6 @@ struct GenShape {
 };
 
 
-// Chunk swizzle of a row-major value tile read through LDS transpose reads:
-// a read pass covers 4 consecutive rows (keys) at 4 consecutive chunks, so
-// the key moves rows by 64 bytes within each 256-byte bank window.
-template <int NC>
-__device__ __forceinline__ int vtr_swz(int r, int c) {
-  static_assert(NC == 8 || NC >= 16, "rows of 128 bytes or of 256 bytes and more");
-  return NC == 8 ? c ^ (((r >> 1) & 1) * 4) : c ^ ((r & 3) * 4);
-}
-
-
 // One softmax over the keys lo .. hi (inclusive, per lane; hi < lo: none) of
 // the 64-key tiles t_first .. t_last. Keys come from kp (rows of DH, nkeys
 // readable rows), values from vtp (DH rows of stride ld_v). The wave's 32

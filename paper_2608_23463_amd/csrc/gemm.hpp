@@ -721,15 +721,6 @@ struct DirectShape {
   static_assert(kLdsBytes <= 160 * 1024, "LDS budget of one workgroup");
 };
 
-typedef short pf_v4i16 __attribute__((ext_vector_type(4)));
-// LDS transpose read: within each 16-lane group, lane i supplies the address
-// of 4 consecutive 16-bit elements and lane l receives element l % 4 of the
-// lanes l / 4, 4 + l / 4, 8 + l / 4, 12 + l / 4, in that order.
-__device__ __forceinline__ pf_v4i16 lds_read_tr16(const void* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) pf_v4i16*)(const_cast<void*>(p)));
-}
-
 // Waits until at most `pending` stages of loads (kLoads each) are in flight.
 template <int L, int NP>
 __device__ __forceinline__ void wait_stages(int pending) {

@@ -64,12 +64,14 @@ hipError_t launch_qk_backward(const HeadsDims& d, const HeadsWeights& w, int64_t
 // queries sees are cut into at most `slices` runs of at least `min_tiles`
 // tiles, by its own length.
 struct PagedPlan {
+  bool prompt;       // paged_prompt_kernel, or the one for single tokens
+  int cols, tile_rows;
   int slices, min_tiles;
   int64_t groups;  // workgroups per slice
   size_t bytes;
 };
-PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragged, int64_t max_kv_len, int64_t window,
-                     int64_t sinks);
+PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragged, int64_t max_new, int64_t max_kv_len,
+                     int64_t window, int64_t sinks);
 hipError_t launch_paged_attention(const HeadsDims& d, const PagedDims& c, const PagedPlan& pl, int64_t n_tokens,
                                   const int32_t* cu_tokens, const Rows& q, float scale, int64_t window, int64_t sinks,
                                   void* out, float* lse, char* ws, hipStream_t s);

@@ -1,0 +1,111 @@
+// What the kernels of attention over a paged cache share: the call's
+// parameters, which rows a block of queries sees, and the join of slices.
+#pragma once
+
+#include "heads.hpp"
+
+namespace pf {
+
+constexpr int kBlock = 16;      // rows per block: a page is a multiple of it
+constexpr int kMaxSlices = 512;
+
+struct PagedParams {
+  const char* q;
+  int64_t q_ts, q_hs;
+  const char* k;
+  const char* v;
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* cu;    // NULL: one token of every sequence
+  int n_pages, page_size, max_pages, batch, n_tokens;
+  FastDiv page_blocks;  // blocks per page
+  int hq, hk, group;
+  FastDiv fgroup, fhk, fslices;
+  int cols, tile_rows;  // queries of a workgroup, rows of a tile (both powers of two)
+  int slices, min_tiles;
+  int window, sinks;    // window: INT32_MAX without one
+  float scale_log2;
+  void* out;
+  float* lse;
+  float* part_o;        // [n_tokens * hq, slices, D]
+  float2* part_ml;      // [n_tokens * hq, slices]
+};
+
+// The new tokens of one sequence. Column x of a (sequence, K/V head) is token
+// x / group, head x % group of the group.
+struct Sequence {
+  int seq;       // -1: none
+  int t0;        // its first token in the call
+  int cols;
+  int row0;      // row of that token
+  int most;      // rows that the table holds
+  __device__ __forceinline__ void set(const PagedParams& p, int s) {
+    seq = s;
+    int n_new = 1;
+    t0 = s;
+    if (p.cu) {
+      t0 = p.cu[s];
+      n_new = p.cu[s + 1] - t0;
+      if (t0 < 0 || n_new <= 0 || n_new > p.n_tokens - t0) {  // nothing there, or boundaries that are none
+        seq = -1;
+        n_new = 0;
+      }
+    }
+    cols = n_new * p.group;
+    const int64_t first = (int64_t)p.kv_len[s] - n_new;
+    row0 = (int)(first < -n_new ? -n_new : first);
+    most = p.max_pages * p.page_size;
+  }
+};
+
+// Blocks of COLS columns: sequence s takes blocks cu[s] * group / COLS + s on,
+// at least as many as its columns fill, so a block finds its sequence without
+// a sum over the others.
+template <int COLS>
+__device__ __forceinline__ int first_block(const PagedParams& p, int s) {
+  return p.cu ? (int)((int64_t)p.cu[s] * p.group / COLS) + s : s * ((p.group + COLS - 1) / COLS);
+}
+// Their number (n_tokens < 0: one token of every sequence).
+inline int64_t col_blocks(int cols, int group, int64_t n_tokens, int batch) {
+  return n_tokens < 0 ? (int64_t)batch * ((group + cols - 1) / cols) : n_tokens * group / cols + batch;
+}
+
+// The largest s < batch with at(s) <= x, counted by the wave, 64 at a time
+// (at rises with s, at(0) <= x).
+template <class F>
+__device__ __forceinline__ int find_sequence(int batch, F&& at, int64_t x) {
+  int s = 0;
+  for (int i = 1; i < batch; i += kWave) {
+    const int c = i + (int)(threadIdx.x & (kWave - 1));
+    s += __popcll(__ballot(c < batch && at(c < batch ? c : 0) <= x));
+  }
+  return __builtin_amdgcn_readfirstlane(s);
+}
+
+// The rows that a block of columns sees, as a list of tiles: those of the
+// first rows, then those of the windows.
+struct Sight {
+  int first, last;  // rows of its first and last token (last = -1: it sees none)
+  int head_tiles;   // tiles that hold the first rows
+  int gap;          // added to later tile numbers
+  int tiles;
+  __device__ __forceinline__ Sight(const PagedParams& p, const Sequence& sq, int x0, int cols, int tile_rows) {
+    first = max(sq.row0 + p.fgroup.div(x0), 0);
+    last = max(min(sq.row0 + p.fgroup.div(x0 + cols - 1), sq.most - 1), -1);
+    const int lo = max(first - p.window + 1, 0), n = last + 1;
+    head_tiles = (min(p.sinks, lo) + tile_rows - 1) / tile_rows;
+    gap = max(lo / tile_rows - head_tiles, 0);
+    tiles = max((n + tile_rows - 1) / tile_rows - gap, 0);
+  }
+  __device__ __forceinline__ int tile(int i) const { return i < head_tiles ? i : i + gap; }
+  __device__ __forceinline__ int per_slice(const PagedParams& p) const {
+    const int even = (tiles + p.slices - 1) / p.slices;
+    return even > p.min_tiles ? even : p.min_tiles;
+  }
+};
+
+// The rows that the attention of n_tokens tokens writes for prompts of bf16;
+// slices > 1 leaves partial results for the join.
+hipError_t launch_paged_prompt(const PagedParams& p, int d, int64_t groups, hipStream_t s);
+
+}  // namespace pf

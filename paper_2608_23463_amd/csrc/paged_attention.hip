@@ -27,7 +27,7 @@
 //    channel VE m + e. In bf16 one permute joins two rows of a channel.
 #include <algorithm>
 
-#include "heads.hpp"
+#include "paged.hpp"
 #include "trace.hpp"
 
 namespace pf {
@@ -36,97 +36,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kBlock = 16;      // rows per block: a page is a multiple of it
-constexpr int kCols = 16;       // queries of a workgroup
-constexpr int kMaxSlices = 512;
-
-struct PagedParams {
-  const char* q;
-  int64_t q_ts, q_hs;
-  const char* k;
-  const char* v;
-  const int32_t* table;
-  const int32_t* kv_len;
-  const int32_t* cu;    // NULL: one token of every sequence
-  int n_pages, page_size, max_pages, batch, n_tokens;
-  FastDiv page_blocks;  // blocks per page
-  int hq, hk, group;
-  FastDiv fgroup, fhk, fslices;
-  int slices, min_tiles;
-  int window, sinks;    // window: INT32_MAX without one
-  float scale_log2;
-  void* out;
-  float* lse;
-  float* part_o;        // [n_tokens * hq, slices, D]
-  float2* part_ml;      // [n_tokens * hq, slices]
-};
-
-// The new tokens of one sequence. Column x of a (sequence, K/V head) is token
-// x / group, head x % group of the group.
-struct Sequence {
-  int seq;       // -1: none
-  int t0;        // its first token in the call
-  int cols;
-  int row0;      // row of that token
-  int most;      // rows that the table holds
-  __device__ __forceinline__ void set(const PagedParams& p, int s) {
-    seq = s;
-    int n_new = 1;
-    t0 = s;
-    if (p.cu) {
-      t0 = p.cu[s];
-      n_new = p.cu[s + 1] - t0;
-      if (t0 < 0 || n_new <= 0 || n_new > p.n_tokens - t0) {  // nothing there, or boundaries that are none
-        seq = -1;
-        n_new = 0;
-      }
-    }
-    cols = n_new * p.group;
-    const int64_t first = (int64_t)p.kv_len[s] - n_new;
-    row0 = (int)(first < -n_new ? -n_new : first);
-    most = p.max_pages * p.page_size;
-  }
-};
-
-// Sequence s takes blocks cu[s] * group / 16 + s on, at least as many as its
-// columns fill, so a block finds its sequence without a sum over the others.
-__device__ __forceinline__ int first_block(const PagedParams& p, int s) {
-  return p.cu ? (int)((int64_t)p.cu[s] * p.group / kCols) + s : s * ((p.group + kCols - 1) / kCols);
-}
-
-// The largest s < batch with at(s) <= x, counted by the wave, 64 at a time
-// (at rises with s, at(0) <= x).
-template <class F>
-__device__ __forceinline__ int find_sequence(int batch, F&& at, int64_t x) {
-  int s = 0;
-  for (int i = 1; i < batch; i += kWave) {
-    const int c = i + (int)(threadIdx.x & (kWave - 1));
-    s += __popcll(__ballot(c < batch && at(c < batch ? c : 0) <= x));
-  }
-  return __builtin_amdgcn_readfirstlane(s);
-}
-
-// The rows that a block of columns sees, as a list of tiles: those of the
-// first rows, then those of the windows.
-struct Sight {
-  int first, last;  // rows of its first and last token (last = -1: it sees none)
-  int head_tiles;   // tiles that hold the first rows
-  int gap;          // added to later tile numbers
-  int tiles;
-  __device__ __forceinline__ Sight(const PagedParams& p, const Sequence& sq, int x0, int cols, int tile_rows) {
-    first = max(sq.row0 + p.fgroup.div(x0), 0);
-    last = max(min(sq.row0 + p.fgroup.div(x0 + cols - 1), sq.most - 1), -1);
-    const int lo = max(first - p.window + 1, 0), n = last + 1;
-    head_tiles = (min(p.sinks, lo) + tile_rows - 1) / tile_rows;
-    gap = max(lo / tile_rows - head_tiles, 0);
-    tiles = max((n + tile_rows - 1) / tile_rows - gap, 0);
-  }
-  __device__ __forceinline__ int tile(int i) const { return i < head_tiles ? i : i + gap; }
-  __device__ __forceinline__ int per_slice(const PagedParams& p) const {
-    const int even = (tiles + p.slices - 1) / p.slices;
-    return even > p.min_tiles ? even : p.min_tiles;
-  }
-};
+constexpr int kCols = 16;  // queries of a workgroup
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -264,10 +174,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(PagedParam
   int up = p.fslices.div(id);
   const int slice = id - up * p.slices;
   const int blk = p.fhk.div(up), hk = up - blk * p.hk;
-  const int s = find_sequence(p.batch, [&](int c) { return first_block(p, c); }, blk);
+  const int s = find_sequence(p.batch, [&](int c) { return first_block<kCols>(p, c); }, blk);
   Sequence sq;
   sq.set(p, s);
-  const int x0 = (blk - first_block(p, s)) * kCols;
+  const int x0 = (blk - first_block<kCols>(p, s)) * kCols;
   if (sq.seq < 0 || x0 < 0 || x0 >= sq.cols) return;
   const int cols = min(sq.cols - x0, kCols);
   const Sight sight(p, sq, x0, cols, TR);
@@ -443,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(PagedParam
 
 // Joins the slices of a (token, head) in a fixed order: a lane per four
 // channels, the streams of slices joined through LDS.
-template <typename T, int D, int TR>
+template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
   constexpr int C4 = D / 4, NS = kThreads / C4;
   __shared__ float so[NS][D];
@@ -454,8 +364,8 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
   sq.set(p, s0);
   const int x = (tok - sq.t0) * p.group + head;
   if (sq.seq < 0 || x < 0 || x >= sq.cols) return;  // behind the last sequence
-  const int x0 = p.cu ? x / kCols * kCols : head / kCols * kCols;
-  const Sight sight(p, sq, x0, min(sq.cols - x0, kCols), TR);
+  const int x0 = x & -p.cols;  // its block's first column
+  const Sight sight(p, sq, x0, min(sq.cols - x0, p.cols), p.tile_rows);
   const int per = sight.per_slice(p);
   const int live = (sight.tiles + per - 1) / per;
   const float2* ml = p.part_ml + (int64_t)row * p.slices;
@@ -492,45 +402,48 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
   }
 }
 
-// Blocks of columns of a call (n_tokens < 0: one token of every sequence).
-int64_t col_blocks(int group, int64_t n_tokens, int batch) {
-  return n_tokens < 0 ? (int64_t)batch * ((group + kCols - 1) / kCols) : n_tokens * group / kCols + batch;
-}
-
-int tile_rows(const HeadsDims& d) { return kBlock * (d.esize == 4 && d.d == 128 ? 1 : 2); }
-
 template <typename T, int D>
-hipError_t attention_on(const PagedParams& p, hipStream_t s) {
+hipError_t attention_on(const PagedParams& p, const PagedPlan& pl, hipStream_t s) {
   const bool tr = trace_on();
-  const unsigned groups = (unsigned)((int64_t)col_blocks(p.group, p.cu ? p.n_tokens : -1, p.batch) * p.hk * p.slices);
-  if (tr) trace_begin("paged_attention", s);
-  paged_attention_kernel<T, D><<<dim3(groups), kThreads, 0, s>>>(p);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (tr) trace_begin(pl.prompt ? "paged_prompt" : "paged_attention", s);
+  if (pl.prompt) {
+    e = launch_paged_prompt(p, D, pl.groups, s);
+  } else {
+    paged_attention_kernel<T, D><<<dim3((unsigned)(pl.groups * pl.slices)), kThreads, 0, s>>>(p);
+    e = hipGetLastError();
+  }
   if (tr) trace_end(s);
   if (e != hipSuccess || p.slices == 1) return e;
   if (tr) trace_begin("paged_join", s);
-  paged_join_kernel<T, D, Tile<T, D>::NB * kBlock><<<dim3((unsigned)(p.n_tokens * p.hq)), kThreads, 0, s>>>(p);
+  paged_join_kernel<T, D><<<dim3((unsigned)(p.n_tokens * p.hq)), kThreads, 0, s>>>(p);
   e = hipGetLastError();
   if (tr) trace_end(s);
   return e;
 }
 
+constexpr int64_t kPromptTokens = 32;  // new tokens of a sequence from which the prompt kernel runs
+
 }  // namespace
 
-PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragged, int64_t max_kv_len, int64_t window,
-                     int64_t sinks) {
-  // Enough workgroups to keep every CU's loads in flight, slices of no less
-  // than a tile per wave.
-  const int tr = tile_rows(d);
+PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragged, int64_t max_new, int64_t max_kv_len,
+                     int64_t window, int64_t sinks) {
+  PagedPlan pl;
+  pl.prompt = d.esize == 2 && ragged && max_new >= kPromptTokens;
+  pl.cols = pl.prompt ? 128 : kCols;
+  pl.tile_rows = pl.prompt ? 64 : kBlock * (d.esize == 4 && d.d == 128 ? 1 : 2);
+  // Enough workgroups to keep every CU busy, slices of no less than a tile per
+  // wave (single tokens) or eight tiles (prompts).
+  pl.min_tiles = pl.prompt ? 8 : kWaves;
+  const int64_t want = pl.prompt ? 512 : 2048;
   window = std::min<int64_t>(window, INT32_MAX);
   sinks = std::min<int64_t>(sinks, INT32_MAX);
+  max_new = std::min<int64_t>(max_new, n_tokens);
   int64_t rows = std::min<int64_t>(max_kv_len, INT32_MAX);
-  if (window > 0 && rows > window + sinks + 2 * tr) rows = window + sinks + 2 * tr;
-  const int64_t tiles = std::max<int64_t>(1, (rows + tr - 1) / tr);
-  PagedPlan pl;
-  pl.min_tiles = kWaves;
-  pl.groups = col_blocks(d.hq / d.hk, ragged ? n_tokens : -1, batch) * d.hk;
-  int64_t s = std::min<int64_t>((2048 + pl.groups - 1) / pl.groups, (tiles + pl.min_tiles - 1) / pl.min_tiles);
+  if (window > 0) rows = std::min(rows, window + sinks + std::min<int64_t>(max_new, pl.cols) + 2 * pl.tile_rows);
+  const int64_t tiles = std::max<int64_t>(1, (rows + pl.tile_rows - 1) / pl.tile_rows);
+  pl.groups = col_blocks(pl.cols, d.hq / d.hk, ragged ? n_tokens : -1, batch) * d.hk;
+  int64_t s = std::min<int64_t>((want + pl.groups - 1) / pl.groups, (tiles + pl.min_tiles - 1) / pl.min_tiles);
   s = std::max<int64_t>(1, std::min<int64_t>(s, kMaxSlices));
   pl.slices = (int)s;
   pl.bytes = s == 1 ? 0 : (size_t)n_tokens * d.hq * s * (d.d * sizeof(float) + sizeof(float2));
@@ -559,6 +472,8 @@ hipError_t launch_paged_attention(const HeadsDims& d, const PagedDims& c, const 
   p.hq = d.hq;
   p.hk = d.hk;
   p.group = d.hq / d.hk;
+  p.cols = pl.cols;
+  p.tile_rows = pl.tile_rows;
   p.slices = pl.slices;
   p.min_tiles = pl.min_tiles;
   p.fslices = FastDiv(pl.slices);
@@ -571,8 +486,8 @@ hipError_t launch_paged_attention(const HeadsDims& d, const PagedDims& c, const 
   p.lse = lse;
   p.part_o = reinterpret_cast<float*>(ws);
   p.part_ml = reinterpret_cast<float2*>(ws + (size_t)n_tokens * d.hq * pl.slices * d.d * sizeof(float));
-  if (d.esize == 2) return d.d == 64 ? attention_on<bf16, 64>(p, s) : attention_on<bf16, 128>(p, s);
-  return d.d == 64 ? attention_on<float, 64>(p, s) : attention_on<float, 128>(p, s);
+  if (d.esize == 2) return d.d == 64 ? attention_on<bf16, 64>(p, pl, s) : attention_on<bf16, 128>(p, pl, s);
+  return d.d == 64 ? attention_on<float, 64>(p, pl, s) : attention_on<float, 128>(p, pl, s);
 }
 
 }  // namespace pf
