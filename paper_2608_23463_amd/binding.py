@@ -606,12 +606,13 @@ def _heads_dtype(cfg):
 
 
 def _want(name, t, dtype, device, shape, contiguous=True):
-    """A device tensor of a call: type, place and shape (None: any size)."""
+    """Data pointer of a tensor of a call, whose type, place and shape (None:
+    any size) are as told."""
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.device != device or not t.is_cuda:
+    if t.device != device:
         raise ValueError(f"{name} must be on the call's GPU {device}, got {t.device}")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+    if t.shape != shape and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -649,30 +650,24 @@ def _positions(cfg, positions, n, device):
     return _want("positions", positions, torch.int32, device, (cfg.n_axes, n))
 
 
-class _On:
-    """The call's GPU as the current one, with `stream` (None: its current
-    stream) as the one that buffers are allocated on and kernels launched to."""
-
-    def __init__(self, device, stream):
-        import torch
-        if device.type != "cuda":
-            raise ValueError(f"tensors must be on a GPU, got {device}")
-        if stream is not None and stream.device != device:
+def _elsewhere(device, stream):
+    """None where a call on `device` with `stream` (None: the current one) can
+    go out as it is; else the context that makes that GPU and stream current,
+    for kernels and for buffers allocated on the way."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, got {device}")
+    if stream is not None:
+        if stream.device != device:
             raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
-        self.ctx = torch.cuda.stream(stream) if stream is not None else None
-        if self.ctx is None and device.index != torch.cuda.current_device():
-            self.ctx = torch.cuda.device(device)
-        self.device = device
+        return torch.cuda.stream(stream)
+    return None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
-    def __enter__(self):
-        import torch
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
 
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+def _current(device) -> int:
+    """The device's current stream."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def qk_norm_rope_forward(cfg: PfHeadsConfig, weights: Dict[str, object], q, k, positions=None, q_out=None, k_out=None,
@@ -681,17 +676,19 @@ def qk_norm_rope_forward(cfg: PfHeadsConfig, weights: Dict[str, object], q, k, p
     normed per head and turned by positions (int32 [n_axes, T] or [T]);
     weights {"gamma_q", "gamma_k", "freqs"}. Returns (q_out, k_out)."""
     dev, n = q.device, q.shape[0]
-    with _On(dev, stream) as s:
-        w = _heads_weights(cfg, weights, dev)
-        rq, rk = _rows(cfg, "q", q, n, cfg.n_heads, dev), _rows(cfg, "k", k, n, cfg.n_kv_heads, dev)
-        at = _positions(cfg, positions, n, dev)
-        if q_out is None:
-            q_out = _empty(q.shape, q.dtype, dev)
-        if k_out is None:
-            k_out = _empty(k.shape, k.dtype, dev)
-        ro, rp = _rows(cfg, "q_out", q_out, n, cfg.n_heads, dev), _rows(cfg, "k_out", k_out, n, cfg.n_kv_heads, dev)
-        _check(load().proxy_qk_norm_rope_forward(ctypes.byref(cfg), ctypes.byref(w), n, ctypes.byref(rq),
-                                                 ctypes.byref(rk), at, ctypes.byref(ro), ctypes.byref(rp), s))
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return qk_norm_rope_forward(cfg, weights, q, k, positions, q_out, k_out)
+    w = _heads_weights(cfg, weights, dev)
+    rq, rk = _rows(cfg, "q", q, n, cfg.n_heads, dev), _rows(cfg, "k", k, n, cfg.n_kv_heads, dev)
+    at = _positions(cfg, positions, n, dev)
+    if q_out is None:
+        q_out = _empty(q.shape, q.dtype, dev)
+    if k_out is None:
+        k_out = _empty(k.shape, k.dtype, dev)
+    ro, rp = _rows(cfg, "q_out", q_out, n, cfg.n_heads, dev), _rows(cfg, "k_out", k_out, n, cfg.n_kv_heads, dev)
+    _check(load().proxy_qk_norm_rope_forward(cfg, w, n, rq, rk, at, ro, rp, _current(dev)))
     return q_out, k_out
 
 
@@ -701,34 +698,33 @@ def qk_norm_rope_backward(cfg: PfHeadsConfig, weights: Dict[str, object], q, k, 
     gains (fp32; None without a norm). q and k are the forward's inputs."""
     import torch
     dev, n = dq_out.device, dq_out.shape[0]
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return qk_norm_rope_backward(cfg, weights, q, k, positions, dq_out, dk_out, dq, dk, workspace)
+    lib = load()
     norm = cfg.norm == PF_NORM_RMS
-    with _On(dev, stream) as s:
-        lib = load()
-        w = _heads_weights(cfg, weights, dev)
-        if norm:
-            rq, rk = _rows(cfg, "q", q, n, cfg.n_heads, dev), _rows(cfg, "k", k, n, cfg.n_kv_heads, dev)
-        else:
-            rq = rk = PfRows(None, 0, 0)
-        at = _positions(cfg, positions, n, dev)
-        ro = _rows(cfg, "dq_out", dq_out, n, cfg.n_heads, dev)
-        rp = _rows(cfg, "dk_out", dk_out, n, cfg.n_kv_heads, dev)
-        if dq is None:
-            dq = _empty(dq_out.shape, dq_out.dtype, dev)
-        if dk is None:
-            dk = _empty(dk_out.shape, dk_out.dtype, dev)
-        gq = gk = None
-        ws, ws_bytes = None, 0
-        if norm:
-            gains = _empty((2, cfg.head_dim), torch.float32, dev)
-            gq, gk = gains[0], gains[1]
-            ws_bytes = int(lib.proxy_qk_workspace_size(ctypes.byref(cfg), n))
-            if workspace is None:
-                workspace = _bytes(ws_bytes, dev)
-            ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        da, db = _rows(cfg, "dq", dq, n, cfg.n_heads, dev), _rows(cfg, "dk", dk, n, cfg.n_kv_heads, dev)
-        _check(lib.proxy_qk_norm_rope_backward(ctypes.byref(cfg), ctypes.byref(w), n, ctypes.byref(rq),
-                                               ctypes.byref(rk), at, ctypes.byref(ro), ctypes.byref(rp),
-                                               ctypes.byref(da), ctypes.byref(db), _ptr(gq), _ptr(gk), ws, ws_bytes, s))
+    w = _heads_weights(cfg, weights, dev)
+    rq = rk = None
+    if norm:
+        rq, rk = _rows(cfg, "q", q, n, cfg.n_heads, dev), _rows(cfg, "k", k, n, cfg.n_kv_heads, dev)
+    at = _positions(cfg, positions, n, dev)
+    ro = _rows(cfg, "dq_out", dq_out, n, cfg.n_heads, dev)
+    rp = _rows(cfg, "dk_out", dk_out, n, cfg.n_kv_heads, dev)
+    if dq is None:
+        dq = _empty(dq_out.shape, dq_out.dtype, dev)
+    if dk is None:
+        dk = _empty(dk_out.shape, dk_out.dtype, dev)
+    da, db = _rows(cfg, "dq", dq, n, cfg.n_heads, dev), _rows(cfg, "dk", dk, n, cfg.n_kv_heads, dev)
+    gq = gk = None
+    ws, ws_bytes = None, 0
+    if norm:
+        gq, gk = _empty((2, cfg.head_dim), torch.float32, dev).unbind()
+        if workspace is None:
+            workspace = _bytes(int(lib.proxy_qk_workspace_size(cfg, n)), dev)
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib.proxy_qk_norm_rope_backward(cfg, w, n, rq, rk, at, ro, rp, da, db, _ptr(gq), _ptr(gk), ws, ws_bytes,
+                                           _current(dev)))
     return dq, dk, gq, gk
 
 
@@ -743,6 +739,8 @@ class PagedCache:
     def __init__(self, cfg: PfHeadsConfig, weights: Dict[str, object], k_pages, v_pages, page_table, kv_len):
         import torch
         dev, dt = k_pages.device, _heads_dtype(cfg)
+        if dev.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU, got {dev}")
         shape = (k_pages.shape[0], cfg.n_kv_heads, None, cfg.head_dim)
         batch = kv_len.shape[0]
         self.cfg = cfg
@@ -764,20 +762,22 @@ class PagedCache:
         q_out of your own where that can be."""
         import torch
         cfg, dev, n = self.cfg, self.device, k.shape[0]
-        with _On(dev, stream) as s:
-            rk, rv = _rows(cfg, "k", k, n, cfg.n_kv_heads, dev), _rows(cfg, "v", v, n, cfg.n_kv_heads, dev)
-            cu = None if cu_tokens is None else _want("cu_tokens", cu_tokens, torch.int32, dev, (self.batch + 1,))
-            at = _positions(cfg, positions, n, dev)
-            rq = ro = None
-            if q is not None:
-                rq = _rows(cfg, "q", q, n, cfg.n_heads, dev)
-                if q_out is None:
-                    q_out = _empty(q.shape, q.dtype, dev)
-                ro = _rows(cfg, "q_out", q_out, n, cfg.n_heads, dev)
-            elif q_out is not None:
-                raise ValueError("q_out without q")
-            _check(load().proxy_paged_append(ctypes.byref(cfg), ctypes.byref(self.wstruct), ctypes.byref(self.state),
-                                             n, cu, rq, ctypes.byref(rk), ctypes.byref(rv), at, ro, s))
+        ctx = _elsewhere(dev, stream)
+        if ctx is not None:
+            with ctx:
+                return self.append(k, v, q, cu_tokens, positions, q_out)
+        rk, rv = _rows(cfg, "k", k, n, cfg.n_kv_heads, dev), _rows(cfg, "v", v, n, cfg.n_kv_heads, dev)
+        cu = None if cu_tokens is None else _want("cu_tokens", cu_tokens, torch.int32, dev, (self.batch + 1,))
+        at = _positions(cfg, positions, n, dev)
+        rq = ro = None
+        if q is not None:
+            rq = _rows(cfg, "q", q, n, cfg.n_heads, dev)
+            if q_out is None:
+                q_out = _empty(q.shape, q.dtype, dev)
+            ro = _rows(cfg, "q_out", q_out, n, cfg.n_heads, dev)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        _check(load().proxy_paged_append(cfg, self.wstruct, self.state, n, cu, rq, rk, rv, at, ro, _current(dev)))
         return q_out
 
     def attend(self, q, max_kv_len: int, cu_tokens=None, max_new: Optional[int] = None, window: int = 0,
@@ -791,25 +791,27 @@ class PagedCache:
         rows of tokens behind the last sequence are left alone."""
         import torch
         cfg, dev, n = self.cfg, self.device, q.shape[0]
+        ctx = _elsewhere(dev, stream)
+        if ctx is not None:
+            with ctx:
+                return self.attend(q, max_kv_len, cu_tokens, max_new, window, sinks, scale, out, lse, workspace)
+        lib = load()
         if max_new is None:
             max_new = 1 if cu_tokens is None else max(n, 1)
-        with _On(dev, stream) as s:
-            lib = load()
-            rq = _rows(cfg, "q", q, n, cfg.n_heads, dev)
-            cu = None if cu_tokens is None else _want("cu_tokens", cu_tokens, torch.int32, dev, (self.batch + 1,))
-            shape = (n, cfg.n_heads, cfg.head_dim)
-            if out is None:
-                out = _empty(shape, q.dtype, dev)
-            to = _want("out", out, q.dtype, dev, shape)
-            tl = None if lse is None else _want("lse", lse, torch.float32, dev, (n, cfg.n_heads))
-            if workspace is None:
-                need = int(lib.proxy_paged_workspace_size(ctypes.byref(cfg), self.batch, n, cu is not None, max_new,
-                                                          max_kv_len, window, sinks))
-                workspace = _bytes(need, dev) if need else None
-            ws, ws_bytes = None, 0
-            if workspace is not None:
-                ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-            _check(lib.proxy_paged_attention(ctypes.byref(cfg), ctypes.byref(self.state), n, cu, rq, max_new,
-                                             max_kv_len, window, sinks,
-                                             cfg.head_dim ** -0.5 if scale is None else scale, to, tl, ws, ws_bytes, s))
+        rq = _rows(cfg, "q", q, n, cfg.n_heads, dev)
+        cu = None if cu_tokens is None else _want("cu_tokens", cu_tokens, torch.int32, dev, (self.batch + 1,))
+        shape = (n, cfg.n_heads, cfg.head_dim)
+        if out is None:
+            out = _empty(shape, q.dtype, dev)
+        to = _want("out", out, q.dtype, dev, shape)
+        tl = None if lse is None else _want("lse", lse, torch.float32, dev, (n, cfg.n_heads))
+        if workspace is None:
+            need = lib.proxy_paged_workspace_size(cfg, self.batch, n, cu is not None, max_new, max_kv_len, window, sinks)
+            workspace = _bytes(need, dev) if need else None
+        ws, ws_bytes = None, 0
+        if workspace is not None:
+            ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check(lib.proxy_paged_attention(cfg, self.state, n, cu, rq, max_new, max_kv_len, window, sinks,
+                                         cfg.head_dim ** -0.5 if scale is None else scale, to, tl, ws, ws_bytes,
+                                         _current(dev)))
         return out

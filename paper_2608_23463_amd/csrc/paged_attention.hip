@@ -40,6 +40,18 @@ constexpr int kCols = 16;  // queries of a workgroup
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+// f over the four lanes l % 16, 16 + l % 16, .., the same in each of them.
+template <class F>
+__device__ __forceinline__ float over_rows(float x, F&& f) {
+  uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  uint32_t e = a[0], o = a[1];  // a bit cast takes the elements as values, not the pair's start
+  u = __builtin_bit_cast(uint32_t, f(__builtin_bit_cast(float, e), __builtin_bit_cast(float, o)));
+  const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  e = b[0], o = b[1];
+  return f(__builtin_bit_cast(float, e), __builtin_bit_cast(float, o));
+}
+
 template <typename T, int D>
 struct Tile;
 
@@ -47,6 +59,7 @@ struct Tile;
 template <int D>
 struct Tile<bf16, D> {
   static constexpr int NB = 2, KS = D / 32, VE = D / 16, JJ = 1, NO = VE;
+  static constexpr int kPerCu = D == 64 ? 4 : 3;  // workgroups that fit a CU's registers
   u32x4 k[NB][KS];
   uint32_t v[NB][4][VE / 2];
   __device__ __forceinline__ void load_k(int b, const bf16* row, int g) {
@@ -117,6 +130,7 @@ struct Tile<bf16, D> {
 template <int D>
 struct Tile<float, D> {
   static constexpr int NB = D == 64 ? 2 : 1, KS = D / 16, VE = 4, JJ = D / 64, NO = 4 * JJ;
+  static constexpr int kPerCu = 3;
   f32x4 k[NB][KS];
   f32x4 v[NB][4][JJ];
   __device__ __forceinline__ void load_k(int b, const float* row, int g) {
@@ -163,7 +177,7 @@ struct Tile<float, D> {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(PagedParams p) {
+__global__ void __launch_bounds__(kThreads, (Tile<T, D>::kPerCu)) paged_attention_kernel(PagedParams p) {
   typedef Tile<T, D> Tl;
   constexpr int NB = Tl::NB, TR = NB * kBlock;
   __shared__ float so[kWaves][kCols][D];
@@ -200,117 +214,108 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(PagedParam
   const T* kp = reinterpret_cast<const T*>(p.k);
   const T* vp = reinterpret_cast<const T*>(p.v);
 
-  // Page number and first slot of a block; -1 where the sequence or the table
-  // has none (its rows are then not seen).
-  auto page_of = [&](int blk, int* slot) {
-    *slot = 0;
-    if (blk * kBlock > sight.last) return -1;
-    const int pg = p.page_blocks.div(blk);
-    *slot = (blk - pg * p.page_blocks.d) * kBlock;
-    const int at = __builtin_amdgcn_readfirstlane(table[pg]);
-    return at >= 0 && at < p.n_pages ? at : -1;
+  // A tile's blocks: their table entries as they are, and their first slots.
+  struct Place {
+    int id[NB], slot[NB];
   };
-
   f32x4 o[Tl::NO];
 #pragma unroll
   for (int i = 0; i < Tl::NO; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float mx = -INFINITY, sum = 0.0f;
 
-  struct Place {
-    int page[NB], slot[NB];
-  };
   auto place = [&](int i) {
     Place w;
-    const int t = sight.tile(min(i, last - 1));
-#pragma unroll
-    for (int b = 0; b < NB; ++b) w.page[b] = page_of(t * NB + b, &w.slot[b]);
-    return w;
-  };
-  auto fetch = [&](const Place& w, Tl& t) {
+    const int blk = sight.tile(min(i, last - 1)) * NB;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      // a block without a page reads page 0 instead, whose rows exist
-      const int64_t at = w.page[b] < 0 ? 0 : w.page[b] * page_rows + (int64_t)hk * p.page_size + w.slot[b];
-      const T* kb = kp + at * D;
-      const T* vb = vp + at * D;
-      t.load_k(b, kb + m * D, g);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) t.load_v(b, r, vb + (4 * g + r) * D, m);
+      const int pg = min(p.page_blocks.div(blk + b), p.max_pages - 1);
+      w.slot[b] = (blk + b - p.page_blocks.div(blk + b) * p.page_blocks.d) * kBlock;
+      w.id[b] = table[pg];
     }
+    return w;
   };
-  auto use = [&](int i, const Place& w, Tl& t) {
-    const int row0 = sight.tile(i) * TR;
-    f32x4 sc[NB];
+  // An entry that is no page reads page 0 instead, whose rows exist.
+  auto is_page = [&](int id) { return (unsigned)id < (unsigned)p.n_pages; };
+  auto base = [&](const Place& w, int b) {
+    return ((is_page(w.id[b]) ? w.id[b] : 0) * page_rows + (int64_t)hk * p.page_size + w.slot[b]) * D;
+  };
+  Tl t;
+  auto fetch_k = [&](const Place& w) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) sc[b] = t.scores(b, q);
-    float pr[4 * NB];
+    for (int b = 0; b < NB; ++b) t.load_k(b, kp + base(w, b) + m * D, g);
+  };
+  auto fetch_v = [&](const Place& w) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) pr[4 * b + r] = sc[b][r] * p.scale_log2;
-    bool whole = row0 + TR - 1 <= sight.first && (row0 > sight.last - p.window || row0 + TR <= p.sinks);
+      for (int r = 0; r < 4; ++r) t.load_v(b, r, vp + base(w, b) + (4 * g + r) * D, m);
+  };
+
+  // The next tile's K is on its way from the moment the scores are formed and
+  // its V from the products on, into the registers these leave; table entries
+  // come a tile before that. Past the slice's end its last tile is fetched
+  // again (a cache hit): behind a condition the compiler would have to wait for
+  // every load at the next use.
+  int i = first + wave;
+  if (i < last) {
+    Place w = place(i), next = place(i + kWaves);
+    fetch_k(w);
+    fetch_v(w);
+    while (true) {
+      const int row0 = sight.tile(i) * TR;
+      f32x4 sc[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) whole = whole && w.page[b] >= 0;
-    if (!whole) {
-      // what is not seen counts for nothing, whatever its bits are
+      for (int b = 0; b < NB; ++b) sc[b] = t.scores(b, q);
+      fetch_k(next);
+      const Place after = place(i + 2 * kWaves);
+      float pr[4 * NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = row0 + b * kBlock + 4 * g + r;
-          if (w.page[b] < 0 || j > row || (j <= lo && j >= p.sinks)) pr[4 * b + r] = -INFINITY;
-          if (w.page[b] < 0 || j > sight.last || (j <= sight.first - p.window && j >= p.sinks)) t.zero_v(b, r);
-        }
-    }
-    float top = pr[0];
+        for (int r = 0; r < 4; ++r) pr[4 * b + r] = sc[b][r] * p.scale_log2;
+      bool whole = row0 + TR - 1 <= sight.first && (row0 > sight.last - p.window || row0 + TR <= p.sinks);
 #pragma unroll
-    for (int r = 1; r < 4 * NB; ++r) top = fmaxf(top, pr[r]);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float now = fmaxf(mx, top);
-    const float ref = now == -INFINITY ? 0.0f : now;
-    const float back = fast_exp2(mx - ref);
-    mx = now;
-    float add = 0.0f;
+      for (int b = 0; b < NB; ++b) whole = whole && is_page(w.id[b]);
+      if (!whole) {
+        // what is not seen counts for nothing, whatever its bits are
 #pragma unroll
-    for (int r = 0; r < 4 * NB; ++r) {
-      pr[r] = fast_exp2(pr[r] - ref);
-      add += pr[r];
-    }
-    sum = sum * back + add;
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int k = 0; k < Tl::NO; ++k) o[k] *= back;
-    t.values(pr, o);
-  };
-
-  // The next tile is on its way while this one is multiplied, and its page
-  // numbers came a tile before that. Past the slice's end its last tile is
-  // fetched again (a cache hit): with a load under a condition the compiler
-  // would have to wait for every load at the next use.
-  int i = first + wave;
-  if (i < last) {
-    Tl ta, tb;
-    Place wa = place(i), wb = place(i + kWaves);
-    fetch(wa, ta);
-    while (true) {
-      fetch(wb, tb);
-      const Place wn = place(i + 2 * kWaves);
-      use(i, wa, ta);
+          for (int r = 0; r < 4; ++r) {
+            const int j = row0 + b * kBlock + 4 * g + r;
+            const bool none = !is_page(w.id[b]);
+            if (none || j > row || (j <= lo && j >= p.sinks)) pr[4 * b + r] = -INFINITY;
+            if (none || j > sight.last || (j <= sight.first - p.window && j >= p.sinks)) t.zero_v(b, r);
+          }
+      }
+      float top = pr[0];
+#pragma unroll
+      for (int r = 1; r < 4 * NB; ++r) top = fmaxf(top, pr[r]);
+      top = over_rows(top, [](float a, float b) { return fmaxf(a, b); });
+      const float now = fmaxf(mx, top);
+      const float ref = now == -INFINITY ? 0.0f : now;
+      const float back = fast_exp2(mx - ref);
+      mx = now;
+      float add = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 4 * NB; ++r) {
+        pr[r] = fast_exp2(pr[r] - ref);
+        add += pr[r];
+      }
+      sum = sum * back + add;
+#pragma unroll
+      for (int k = 0; k < Tl::NO; ++k) o[k] *= back;
+      t.values(pr, o);
+      fetch_v(next);
       i += kWaves;
       if (i >= last) break;
-      fetch(wn, ta);
-      const Place wm = place(i + 2 * kWaves);
-      use(i, wb, tb);
-      i += kWaves;
-      if (i >= last) break;
-      wa = wn;
-      wb = wm;
+      w = next;
+      next = after;
     }
   }
 
   // join the four waves
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
+  sum = over_rows(sum, [](float a, float b) { return a + b; });
   if (g == 0) {
     sm[wave][m] = mx;
     sl[wave][m] = sum;
