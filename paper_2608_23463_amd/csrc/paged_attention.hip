@@ -437,10 +437,6 @@ PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragge
   pl.prompt = d.esize == 2 && ragged && max_new >= kPromptTokens;
   pl.cols = pl.prompt ? 128 : kCols;
   pl.tile_rows = pl.prompt ? 64 : kBlock * (d.esize == 4 && d.d == 128 ? 1 : 2);
-  // Enough workgroups to keep every CU busy, slices of no less than a tile per
-  // wave (single tokens) or eight tiles (prompts).
-  pl.min_tiles = pl.prompt ? 8 : kWaves;
-  const int64_t want = pl.prompt ? 512 : 2048;
   window = std::min<int64_t>(window, INT32_MAX);
   sinks = std::min<int64_t>(sinks, INT32_MAX);
   max_new = std::min<int64_t>(max_new, n_tokens);
@@ -448,6 +444,17 @@ PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragge
   if (window > 0) rows = std::min(rows, window + sinks + std::min<int64_t>(max_new, pl.cols) + 2 * pl.tile_rows);
   const int64_t tiles = std::max<int64_t>(1, (rows + pl.tile_rows - 1) / pl.tile_rows);
   pl.groups = col_blocks(pl.cols, d.hq / d.hk, ragged ? n_tokens : -1, batch) * d.hk;
+  // Few groups: two workgroups per CU, if that leaves each enough tiles (fewer
+  // and longer slices stream better: 8 heads over 1M rows take 702 us in 512
+  // workgroups, 729 in 2,048 and 760 in 4,096). Where the groups fill the chip
+  // by themselves, cuts only even out sequences of different lengths, and short
+  // slices cost more than that gives (48 sequences of up to 9,000 rows, 8 heads:
+  // 180 us in 768 workgroups, 159 in slices of 32 tiles; 64 sequences of up to
+  // 1,000 rows, 16 heads: 33 us whole, 41 in slices of 16). A prompt's groups
+  // are compute bound: eight tiles at least.
+  const bool filled = pl.groups >= 256;
+  const int64_t want = pl.prompt || !filled ? 512 : 4096;
+  pl.min_tiles = pl.prompt || pl.groups < 32 ? 8 : filled ? 32 : 16;
   int64_t s = std::min<int64_t>((want + pl.groups - 1) / pl.groups, (tiles + pl.min_tiles - 1) / pl.min_tiles);
   s = std::max<int64_t>(1, std::min<int64_t>(s, kMaxSlices));
   pl.slices = (int)s;

@@ -213,6 +213,9 @@ ONE = {
     "window_33_sinks_5": (8, 2, 128, "bf16", 16, [600, 33, 34, 38, 39, 70], 33, 5),
     "window_100_sinks_70": (4, 4, 64, "fp32", 32, [400, 169, 170, 171, 60], 100, 70),
     "window_past_all": (4, 4, 64, "bf16", 16, [50, 90], 1 << 40, 3),
+    "long_and_short": (6, 2, 128, "bf16", 32, [5000, 3, 0, 2100, 700, 0, 1025, 64], 0, 0),
+    "long_and_short_mha": (3, 3, 64, "bf16", 16, [0, 2000, 1, 4100, 513], 0, 0),
+    "long_and_short_fp32_window": (20, 1, 64, "fp32", 64, [3000, 900, 0, 2000], 1500, 40),
     "many_slots": (2, 1, 64, "bf16", 16, [(37 * i) % 90 for i in range(150)], 0, 0),
 }
 
