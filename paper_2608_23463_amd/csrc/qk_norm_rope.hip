@@ -108,8 +108,7 @@ struct QkParams {
   FastDiv fq, fk;
   float eps;
   int norm;
-  int parts;  // waves that share a token block's passes
-  FastDiv fparts;
+  FastDiv fparts;  // few tokens: waves of a token
   // append
   char* k_pages;
   char* v_pages;
@@ -179,10 +178,18 @@ __device__ __forceinline__ void rotate(float* v, const float2* cs, bool turned, 
   }
 }
 
+// Sum over the 4 or 8 neighbouring lanes of a row, on the VALU: each other
+// lane of a pair, then of the two pairs, then (mirrored) of the two fours.
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
 template <int LPR>
 __device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-  for (int o = 1; o < LPR; o <<= 1) v += __shfl_xor(v, o);
+  static_assert(LPR == 4 || LPR == 8, "lanes of a row");
+  v = add_lane<0xb1>(v);              // quad_perm 1 0 3 2
+  v = add_lane<0x4e>(v);              // quad_perm 2 3 0 1
+  if (LPR == 8) v = add_lane<0x141>(v);  // row_half_mirror
   return v;
 }
 
@@ -208,16 +215,77 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int64_t
   return s;
 }
 
-// KIND 0: forward into tensors; 1: append into pages.
-template <typename T, int D, bool PAIRS, int TPW, int KIND>
+// One tensor's rows of a launch: which = 0 queries, 1 keys, 2 values (append:
+// copied as they are).
+struct Tensor {
+  Rows in, out;
+  const void* gamma;
+  int heads, which;
+  FastDiv fd;
+};
+__device__ __forceinline__ Tensor tensor_of(const QkParams& p, int which) {
+  return which == 0 ? Tensor{p.q, p.q_out, p.gamma_q, p.hq, 0, p.fq}
+                    : which == 1 ? Tensor{p.k, p.k_out, p.gamma_k, p.hk, 1, p.fk} : Tensor{p.v, Rows{}, nullptr, p.hk, 2, p.fk};
+}
+
+template <typename T>
+__device__ __forceinline__ void load_gain(const QkParams& p, const Tensor& x, int a, int b, float* g) {
+  if (!p.norm || x.which == 2) return;
+  if (x.gamma) {
+    load8(static_cast<const T*>(x.gamma) + a, g);
+    load8(static_cast<const T*>(x.gamma) + b, g + 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) g[i] = 1.0f;
+  }
+}
+
+// Norm and rotation of the lane's 16 elements of a row.
+template <int D, bool PAIRS>
+__device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, float* v, const float* g, const float2* cs,
+                                              bool turned) {
+  if (which == 2) return;
+  if (p.norm) {
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ss += v[i] * v[i];
+    const float rstd = rsqrtf(row_sum<D / 16>(ss) * (1.0f / D) + p.eps);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= rstd * g[i];
+  }
+  rotate<PAIRS>(v, cs, turned, 1.0f);
+}
+
+// Where a token of an append goes: its row (head 0) in the pages, or -1 for one
+// behind the last sequence or without a place; `at` is its row of the sequence,
+// kv_len - new + i for the i-th new token.
+__device__ __forceinline__ int64_t place_of(const QkParams& p, int64_t tok, int* at) {
+  const int s = p.cu ? sequence_of(p.cu, p.batch, tok) : (int)tok;
+  *at = 0;
+  if (s >= p.batch) return -1;
+  const int64_t pos = p.cu ? (int64_t)p.kv_len[s] - p.cu[s + 1] + tok : (int64_t)p.kv_len[s] - 1;
+  if (pos < 0 || pos >= (int64_t)p.max_pages * p.page_size) return -1;
+  *at = (int)pos;
+  const int pg = p.fpage.div((int)pos);
+  const int id = p.table[(int64_t)s * p.max_pages + pg];
+  return id >= 0 && id < p.n_pages ? (int64_t)id * p.hk * p.page_size + ((int)pos - pg * p.page_size) : -1;
+}
+
+// Destination of a row of token `tok`, whose place is `place` in an append.
+template <typename T, int D, bool APPEND>
+__device__ __forceinline__ T* destination(const QkParams& p, const Tensor& x, int64_t tok, int h, int64_t place) {
+  if (!APPEND || x.which == 0) return reinterpret_cast<T*>(x.out.p) + tok * x.out.ts + h * x.out.hs;
+  return reinterpret_cast<T*>(x.which == 1 ? p.k_pages : p.v_pages) + (place + (int64_t)h * p.page_size) * D;
+}
+
+// Many tokens: TPW of them per wave, all their rows.
+template <typename T, int D, bool PAIRS, int TPW, bool APPEND>
 __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p) {
   constexpr int LPR = D / 16, RPP = kWave / LPR;  // lanes per row, rows per pass
   __shared__ float2 turns[kWaves][TPW][D / 2];
-  __shared__ int64_t rows[kWaves][TPW];  // append: row (head 0) of each token in a page, or -1
+  __shared__ int64_t places[kWaves][TPW];
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const int unit = (int)(blockIdx.x * kWaves + wave), block = p.fparts.div(unit);
-  const int64_t t0 = (int64_t)block * TPW;
-  const int part = unit - block * p.parts;
+  const int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * TPW;
   const int tokens = (int)min((int64_t)TPW, p.turn.n - t0);
   if (tokens <= 0) return;  // waves share nothing: no barrier below
   const int row = lane / LPR;
@@ -225,26 +293,14 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p) {
 
   for (int i = 0; i < tokens; ++i) {
     int at = 0;
-    if (KIND == 1) {
-      // where the token goes: row kv_len - new + i of its sequence
-      const int64_t tok = t0 + i;
-      const int s = p.cu ? sequence_of(p.cu, p.batch, tok) : (int)tok;
-      int64_t dst = -1;  // behind the last sequence, or without a place: left alone
-      if (s < p.batch) {
-        const int64_t pos = p.cu ? (int64_t)p.kv_len[s] - p.cu[s + 1] + tok : (int64_t)p.kv_len[s] - 1;
-        at = (int)pos;
-        if (pos >= 0 && pos < (int64_t)p.max_pages * p.page_size) {
-          const int pg = p.fpage.div((int)pos);
-          const int id = p.table[(int64_t)s * p.max_pages + pg];
-          if (id >= 0 && id < p.n_pages) dst = (int64_t)id * p.hk * p.page_size + ((int)pos - pg * p.page_size);
-        }
-      }
-      if (lane == 0) rows[wave][i] = dst;
+    if (APPEND) {
+      const int64_t place = place_of(p, t0 + i, &at);
+      if (lane == 0) places[wave][i] = place;
     }
     for (int pair = lane; pair < D / 2; pair += kWave) {
       float2 cs = make_float2(1.0f, 0.0f);
       if (pair < p.turn.rot / 2) {
-        if (KIND == 0 || p.turn.positions) at = position_of(p.turn, t0 + i, axis_of(p.turn, pair));
+        if (!APPEND || p.turn.positions) at = position_of(p.turn, t0 + i, axis_of(p.turn, pair));
         cs = turn_of(p.turn.freqs[pair], at);
       }
       turns[wave][i][pair] = cs;
@@ -252,58 +308,74 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p) {
   }
   __builtin_amdgcn_wave_barrier();  // LDS of the wave's own: in order without a workgroup barrier
 
-  auto run = [&](const Rows& in, const Rows& out, const void* gamma, int heads, const FastDiv& fd, int which) {
-    const int items = tokens * heads;
+  for (int which = p.q.p ? 0 : 1; which < (APPEND ? 3 : 2); ++which) {
+    const Tensor x = tensor_of(p, which);
+    const int items = tokens * x.heads;
     float g[16];
-    if (p.norm && which < 2) {
-      if (gamma) {
-        load8(static_cast<const T*>(gamma) + ch.a, g);
-        load8(static_cast<const T*>(gamma) + ch.b, g + 8);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) g[i] = 1.0f;
-      }
-    }
-    for (int base = part * RPP; base < items; base += p.parts * RPP) {
+    load_gain<T>(p, x, ch.a, ch.b, g);
+    for (int base = 0; base < items; base += RPP) {
       const int it = base + row;
       const bool on = it < items;
-      const int tk = on ? fd.div(it) : 0, h = on ? it - tk * heads : 0;
-      const T* src = reinterpret_cast<const T*>(in.p) + (t0 + tk) * in.ts + h * in.hs;
+      const int tk = on ? x.fd.div(it) : 0, h = on ? it - tk * x.heads : 0;
       float v[16];
       Raw8<T> r[2];
-      load16(src, ch.a, ch.b, r);
+      load16(reinterpret_cast<const T*>(x.in.p) + (t0 + tk) * x.in.ts + h * x.in.hs, ch.a, ch.b, r);
       raw_to_f32(r[0], v);
       raw_to_f32(r[1], v + 8);
-      if (which < 2) {
-        if (p.norm) {
-          float ss = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) ss += v[i] * v[i];
-          const float rstd = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + p.eps);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] *= rstd * g[i];
-        }
-        rotate<PAIRS>(v, &turns[wave][tk][8 * (lane % LPR)], ch.turned, 1.0f);
-      }
-      T* dst;
-      bool write = on;
-      if (KIND == 1) {
-        const int64_t r0 = rows[wave][tk];
-        write = write && r0 >= 0;
-        dst = which == 0 ? reinterpret_cast<T*>(out.p) + (t0 + tk) * out.ts + h * out.hs
-                         : reinterpret_cast<T*>(which == 1 ? p.k_pages : p.v_pages) + (r0 + (int64_t)h * p.page_size) * D;
-      } else {
-        dst = reinterpret_cast<T*>(out.p) + (t0 + tk) * out.ts + h * out.hs;
-      }
-      if (write) {
+      norm_and_turn<D, PAIRS>(p, which, v, g, &turns[wave][tk][8 * (lane % LPR)], ch.turned);
+      const int64_t place = APPEND ? places[wave][tk] : 0;
+      if (on && place >= 0) {
+        T* dst = destination<T, D, APPEND>(p, x, t0 + tk, h, place);
         store8(dst + ch.a, v);
         store8(dst + ch.b, v + 8);
       }
     }
-  };
-  if (p.q.p) run(p.q, p.q_out, p.gamma_q, p.hq, p.fq, 0);
-  run(p.k, p.k_out, p.gamma_k, p.hk, p.fk, 1);
-  if (KIND == 1) run(p.v, p.v, nullptr, p.hk, p.fk, 2);
+  }
+}
+
+// Few tokens: a wave for every RPP rows of every token, whose loads are on
+// their way while it finds the token's place and its turns.
+template <typename T, int D, bool PAIRS, bool APPEND>
+__global__ void __launch_bounds__(kThreads) qk_few_kernel(QkParams p) {
+  constexpr int LPR = D / 16, RPP = kWave / LPR;
+  __shared__ float2 turns[kWaves][D / 2];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int unit = (int)blockIdx.x * kWaves + wave;
+  const int tok = p.fparts.div(unit);
+  int part = unit - tok * p.fparts.d;
+  if (tok >= p.turn.n) return;
+  const int pq = p.q.p ? (p.hq + RPP - 1) / RPP : 0, pk = (p.hk + RPP - 1) / RPP;
+  const int which = part < pq ? 0 : part < pq + pk ? 1 : 2;
+  part -= which == 0 ? 0 : which == 1 ? pq : pq + pk;
+  const Tensor x = tensor_of(p, which);
+  const Chunk<D, PAIRS> ch(lane % LPR, p.turn.rot);
+  const int h = part * RPP + lane / LPR;
+  const bool on = h < x.heads;
+  float g[16], v[16];
+  Raw8<T> r[2];
+  load16(reinterpret_cast<const T*>(x.in.p) + (int64_t)tok * x.in.ts + (on ? h : 0) * x.in.hs, ch.a, ch.b, r);
+  load_gain<T>(p, x, ch.a, ch.b, g);
+  int at = 0;
+  const int64_t place = APPEND ? place_of(p, tok, &at) : 0;
+  if (which < 2) {
+    for (int pair = lane; pair < D / 2; pair += kWave) {
+      float2 cs = make_float2(1.0f, 0.0f);
+      if (pair < p.turn.rot / 2) {
+        if (!APPEND || p.turn.positions) at = position_of(p.turn, tok, axis_of(p.turn, pair));
+        cs = turn_of(p.turn.freqs[pair], at);
+      }
+      turns[wave][pair] = cs;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  raw_to_f32(r[0], v);
+  raw_to_f32(r[1], v + 8);
+  norm_and_turn<D, PAIRS>(p, which, v, g, &turns[wave][8 * (lane % LPR)], ch.turned);
+  if (on && place >= 0) {
+    T* dst = destination<T, D, APPEND>(p, x, tok, h, place);
+    store8(dst + ch.a, v);
+    store8(dst + ch.b, v + 8);
+  }
 }
 
 struct QkBwdParams {
@@ -322,18 +394,25 @@ struct QkBwdParams {
 // dx = rstd (g - xn mean(g xn)). A lane keeps the gains' gradients of its 16
 // elements over all its rows; the workgroups' sums are joined in a fixed order.
 template <typename T, int D, bool PAIRS, int TPW>
-__global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkBwdParams p) {
+__global__ void __launch_bounds__(kThreads, 3) qk_backward_kernel(QkBwdParams p) {
   constexpr int LPR = D / 16, RPP = kWave / LPR;
   __shared__ float2 turns[kWaves][TPW][D / 2];
   __shared__ float sums[kWaves][D];
+  __shared__ float gains[2][D];
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   const int row = lane / LPR;
   const Chunk<D, PAIRS> ch(lane % LPR, p.turn.rot);
   float acc[2][16] = {};
+  for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
+    const T* gamma = static_cast<const T*>(i < D ? p.gamma_q : p.gamma_k);
+    gains[i / D][i % D] = p.norm && gamma ? to_f32(gamma[i % D]) : 1.0f;
+  }
+  __syncthreads();
   const int64_t step = (int64_t)gridDim.x * kWaves * TPW;
   for (int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * TPW; t0 < p.turn.n; t0 += step) {
     const int tokens = (int)min((int64_t)TPW, p.turn.n - t0);
     __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
     for (int i = 0; i < tokens; ++i)
       for (int pair = lane; pair < D / 2; pair += kWave) {
         float2 cs = make_float2(1.0f, 0.0f);
@@ -342,23 +421,12 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkBwdParams p) {
         turns[wave][i][pair] = cs;
       }
     __builtin_amdgcn_wave_barrier();
-    auto run = [&](const Rows& x, const Rows& dy, const Rows& dx, const void* gamma, int heads, const FastDiv& fd,
+    auto run = [&](const Rows& x, const Rows& dy, const Rows& dx, const float* gain, int heads, const FastDiv& fd,
                    float* ac) {
       const int items = tokens * heads;
-      float g[16];
-      if (p.norm) {
-        if (gamma) {
-          load8(static_cast<const T*>(gamma) + ch.a, g);
-          load8(static_cast<const T*>(gamma) + ch.b, g + 8);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) g[i] = 1.0f;
-        }
-      }
-      for (int base = 0; base < items; base += RPP) {
-        const int it = base + row;
-        const bool on = it < items;
-        const int tk = on ? fd.div(it) : 0, h = on ? it - tk * heads : 0;
+#pragma unroll 1
+      for (int it = row; it < items; it += RPP) {  // a row's lanes are on or off together
+        const int tk = fd.div(it), h = it - tk * heads;
         float dz[16];
         Raw8<T> r[2], rx[2];
         load16(reinterpret_cast<const T*>(dy.p) + (t0 + tk) * dy.ts + h * dy.hs, ch.a, ch.b, r);
@@ -374,11 +442,17 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkBwdParams p) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) ss += xn[i] * xn[i];
           const float rstd = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + p.eps);
+          // read here, not kept over the rows: with both tensors' gains in
+          // registers fewer waves fit
+          asm volatile("" ::: "memory");
+          float g[16];
+          load8(gain + ch.a, g);
+          load8(gain + ch.b, g + 8);
           float dot = 0.0f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             xn[i] *= rstd;
-            if (on) ac[i] += dz[i] * xn[i];
+            ac[i] += dz[i] * xn[i];
             dz[i] *= g[i];
             dot += dz[i] * xn[i];
           }
@@ -386,15 +460,13 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkBwdParams p) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) dz[i] = rstd * (dz[i] - xn[i] * mean);
         }
-        if (on) {
-          T* dst = reinterpret_cast<T*>(dx.p) + (t0 + tk) * dx.ts + h * dx.hs;
-          store8(dst + ch.a, dz);
-          store8(dst + ch.b, dz + 8);
-        }
+        T* dst = reinterpret_cast<T*>(dx.p) + (t0 + tk) * dx.ts + h * dx.hs;
+        store8(dst + ch.a, dz);
+        store8(dst + ch.b, dz + 8);
       }
     };
-    run(p.q, p.dqo, p.dq, p.gamma_q, p.hq, p.fq, acc[0]);
-    run(p.k, p.dko, p.dk, p.gamma_k, p.hk, p.fk, acc[1]);
+    run(p.q, p.dqo, p.dq, gains[0], p.hq, p.fq, acc[0]);
+    run(p.k, p.dko, p.dk, gains[1], p.hk, p.fk, acc[1]);
   }
   if (!p.norm || !p.part) return;
 #pragma unroll
@@ -418,20 +490,25 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkBwdParams p) {
 }
 
 // dgamma[w][c] = sum over the workgroups' rows, in a fixed order: 64 columns
-// per workgroup, 16 streams of rows joined through LDS.
+// per workgroup, 16 streams of rows joined through LDS, eight loads in flight
+// in each.
 __global__ void __launch_bounds__(1024) qk_gain_kernel(const float* part, int blocks, int D, float* dgq, float* dgk) {
   __shared__ float sums[16][64];
   const int w = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 63), st = threadIdx.x >> 6;
-  float v = 0.0f;
-  for (int b = st; b < blocks; b += 16) v += part[((int64_t)w * blocks + b) * D + c];
-  sums[st][threadIdx.x & 63] = v;
+  const float* p = part + (int64_t)w * blocks * D + c;
+  float v[8] = {};
+  for (int b = st; b < blocks; b += 16 * 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += b + 16 * i < blocks ? p[(int64_t)(b + 16 * i) * D] : 0.0f;
+  }
+  sums[st][threadIdx.x & 63] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   __syncthreads();
   if (st == 0) {
-    v = 0.0f;
+    float all = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v += sums[i][threadIdx.x];
+    for (int i = 0; i < 16; ++i) all += sums[i][threadIdx.x];
     float* out = w ? dgk : dgq;
-    if (out) out[c] = v;
+    if (out) out[c] = all;
   }
 }
 
@@ -458,37 +535,35 @@ hipError_t timed(const char* label, hipStream_t s, F&& f) {
   return e;
 }
 
-template <typename T, int D, bool PAIRS, int KIND>
+constexpr int64_t kFewTokens = 2048;
+
+template <typename T, int D, bool PAIRS, bool APPEND>
 hipError_t forward_on(QkParams p, int64_t n, const char* label, hipStream_t s) {
-  // few tokens: one per wave and several waves to a token, so that a call of
-  // one token still spreads its heads; many: four per wave
-  const int rows = 64 / (D / 16);
-  const int passes = ((p.q.p && p.hq > p.hk ? p.hq : p.hk) + rows - 1) / rows;
+  constexpr int RPP = kWave / (D / 16);
   return timed(label, s, [&] {
-    if (n < 2048) {
-      p.parts = passes;
-      p.fparts = FastDiv(p.parts);
-      const int64_t units = n * p.parts;
-      qk_forward_kernel<T, D, PAIRS, 1, KIND><<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
+    if (n < kFewTokens) {
+      const int pk = (p.hk + RPP - 1) / RPP;
+      p.fparts = FastDiv((p.q.p ? (p.hq + RPP - 1) / RPP : 0) + (APPEND ? 2 * pk : pk));
+      const int64_t units = n * p.fparts.d;
+      qk_few_kernel<T, D, PAIRS, APPEND><<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
     } else {
-      p.parts = 1;
       const int64_t units = (n + kTokensPerWave - 1) / kTokensPerWave;
-      qk_forward_kernel<T, D, PAIRS, kTokensPerWave, KIND>
+      qk_forward_kernel<T, D, PAIRS, kTokensPerWave, APPEND>
           <<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
     }
   });
 }
 
-template <int KIND>
+template <bool APPEND>
 hipError_t forward_any(const HeadsDims& d, const QkParams& p, int64_t n, const char* label, hipStream_t s) {
   if (d.esize == 2) {
     if (d.d == 64)
-      return d.pairs_style ? forward_on<bf16, 64, true, KIND>(p, n, label, s) : forward_on<bf16, 64, false, KIND>(p, n, label, s);
-    return d.pairs_style ? forward_on<bf16, 128, true, KIND>(p, n, label, s) : forward_on<bf16, 128, false, KIND>(p, n, label, s);
+      return d.pairs_style ? forward_on<bf16, 64, true, APPEND>(p, n, label, s) : forward_on<bf16, 64, false, APPEND>(p, n, label, s);
+    return d.pairs_style ? forward_on<bf16, 128, true, APPEND>(p, n, label, s) : forward_on<bf16, 128, false, APPEND>(p, n, label, s);
   }
   if (d.d == 64)
-    return d.pairs_style ? forward_on<float, 64, true, KIND>(p, n, label, s) : forward_on<float, 64, false, KIND>(p, n, label, s);
-  return d.pairs_style ? forward_on<float, 128, true, KIND>(p, n, label, s) : forward_on<float, 128, false, KIND>(p, n, label, s);
+    return d.pairs_style ? forward_on<float, 64, true, APPEND>(p, n, label, s) : forward_on<float, 64, false, APPEND>(p, n, label, s);
+  return d.pairs_style ? forward_on<float, 128, true, APPEND>(p, n, label, s) : forward_on<float, 128, false, APPEND>(p, n, label, s);
 }
 
 QkParams qk_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, const int32_t* positions) {
@@ -502,12 +577,11 @@ QkParams qk_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, const i
   p.fk = FastDiv(d.hk);
   p.eps = d.eps;
   p.norm = d.norm;
-  p.parts = 1;
   return p;
 }
 
 constexpr int kBwdTokens = 4;      // tokens per wave and step of the backward
-constexpr int kBwdBlocks = 2048;   // workgroups at most (their gain sums are joined)
+constexpr int kBwdBlocks = 1024;   // workgroups at most (their gain sums are joined)
 
 int bwd_blocks(int64_t n) {
   const int64_t per = (int64_t)kWaves * kBwdTokens;
@@ -529,7 +603,7 @@ hipError_t launch_qk_forward(const HeadsDims& d, const HeadsWeights& w, int64_t 
   p.k = k;
   p.q_out = q_out;
   p.k_out = k_out;
-  return forward_any<0>(d, p, n, "qk_norm_rope", s);
+  return forward_any<false>(d, p, n, "qk_norm_rope", s);
 }
 
 hipError_t launch_paged_append(const HeadsDims& d, const HeadsWeights& w, const PagedDims& c, int64_t n,
@@ -550,7 +624,7 @@ hipError_t launch_paged_append(const HeadsDims& d, const HeadsWeights& w, const 
   p.max_pages = c.max_pages;
   p.batch = c.batch;
   p.fpage = FastDiv(c.page_size);
-  return forward_any<1>(d, p, n, "paged_append", s);
+  return forward_any<true>(d, p, n, "paged_append", s);
 }
 
 size_t qk_backward_ws(const HeadsDims& d, int64_t n) {
