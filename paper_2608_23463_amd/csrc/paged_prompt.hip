@@ -33,6 +33,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
   constexpr int kTileBytes = kTile * RB, kStage = 2 * kTileBytes;
   constexpr int kLoads = kBlock * RB / 1024;  // 1 KB loads of a wave's 16 rows
   constexpr int kRowsPerLoad = 1024 / RB;
+  constexpr int kPerTile = kTile / kBlock, kAhead = kWave / kPerTile;
   __shared__ __attribute__((aligned(1024))) char smem[2 * kStage];
 
   // Every XCD takes a contiguous run of (K/V head, block), so the blocks of a
@@ -85,33 +86,28 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
   }
 
   const int32_t* table = p.table + (int64_t)s * p.max_pages;
-  const int64_t page_rows = (int64_t)p.hk * p.page_size;
-  // First row of a block of 16 in the pages, counted over the cache; -1 where
-  // the sequence or the table has none.
-  auto row_of = [&](int blk16) -> int64_t {
-    if (blk16 * kBlock > sight.last) return -1;
-    const int pg = p.page_blocks.div(blk16);
-    const int id = __builtin_amdgcn_readfirstlane(table[pg]);
-    if (id < 0 || id >= p.n_pages) return -1;
-    return id * page_rows + (int64_t)hk * p.page_size + (blk16 - pg * p.page_blocks.d) * kBlock;
-  };
+  const int page_rows = p.hk * p.page_size;  // a cache has fewer than 2^31 rows
   auto tile_row = [&](int t) { return sight.tile(first + t) * kTile; };
-  // Starts the loads of a tile; returns which of its blocks have no page, a
-  // bit each.
-  auto issue = [&](int t, int stage) {
+  // First cache rows of the blocks of 16 tiles, a block per lane: -1 where the
+  // sequence or the table has none. One vector load for 16 tiles, on its way
+  // as long beforehand: scalar lookups per tile would make every wait for an
+  // LDS read wait for them too (with them 8,192 tokens took 637 us, not 546).
+  auto blocks_of = [&](int t) -> int {
+    const int tl = t + lane / kPerTile;
+    const int blk16 = tile_row(min(tl, ntiles - 1)) / kBlock + lane % kPerTile;
+    const int pg = p.page_blocks.div(blk16);
+    const int id = table[min(pg, p.max_pages - 1)];
+    const bool have = blk16 * kBlock <= sight.last && (unsigned)id < (unsigned)p.n_pages;
+    return have ? id * page_rows + hk * p.page_size + (blk16 - pg * p.page_blocks.d) * kBlock : -1;
+  };
+  // Starts the loads of a tile whose blocks are `rows`' from lane `at` on.
+  auto issue = [&](int t, int stage, int rows, int at) {
     const int r0 = tile_row(t);
-    int none = 0;
-    int64_t mine16 = -1;
-#pragma unroll
-    for (int b = 0; b < kTile / kBlock; ++b) {
-      const int64_t at16 = row_of(r0 / kBlock + b);
-      none |= (at16 < 0) << b;
-      if (b == wave) mine16 = at16;
-    }
+    const int mine16 = __builtin_amdgcn_readlane(rows, at + wave);
     // a block without a page, and value rows that no column sees, land as zeros
     const bool all = r0 + kTile - 1 <= sight.first && (r0 > sight.last - p.window || r0 + kTile <= p.sinks);
     const uint32_t bytes = mine16 < 0 ? 0 : kBlock * RB;
-    const int64_t base = mine16 < 0 ? 0 : mine16 * RB;
+    const int64_t base = mine16 < 0 ? 0 : (int64_t)mine16 * RB;
     const rsrc_t rk = make_rsrc_uniform(p.k + base, bytes), rv = make_rsrc_uniform(p.v + base, bytes);
     char* st = smem + stage * kStage + wave * kBlock * RB;
 #pragma unroll
@@ -129,7 +125,6 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
       }
       buf_ld16_lds(rv, off, st + kTileBytes + j * 1024);
     }
-    return none;
   };
 
   f32x16 o[D / 32];
@@ -144,13 +139,22 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
   bool have_ref = false;  // wave-uniform
   constexpr float kSumLimit = 18446744073709551616.0f;  // 2^64
 
-  int none = ntiles > 0 ? issue(0, 0) : 0;
+  int rows = -1, rows_next = -1;  // of 16 tiles, and of the 16 behind them
+  if (ntiles > 0) {
+    rows = blocks_of(0);
+    rows_next = blocks_of(kAhead);
+    issue(0, 0, rows, 0);
+  }
   for (int t = 0; t < ntiles; ++t) {
-    const int r0 = tile_row(t);
+    const int r0 = tile_row(t), in = t % kAhead;
     wait_vmcnt<0>();
     lds_barrier();  // tile t landed for all; every wave is done with tile t - 1
-    const int gone = none;
-    if (t + 1 < ntiles) none = issue(t + 1, (t + 1) & 1);
+    const int gone = (int)(__builtin_amdgcn_ballot_w64(rows < 0) >> (in * kPerTile)) & ((1 << kPerTile) - 1);
+    if (in == kAhead - 1) {
+      rows = rows_next;
+      if (t + 1 + kAhead < ntiles) rows_next = blocks_of(t + 1 + kAhead);
+    }
+    if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1, rows, (t + 1) % kAhead * kPerTile);
     const char* sk = smem + (t & 1) * kStage;
     const char* sv = sk + kTileBytes;
     if (r0 > wlast || (r0 + kTile - 1 <= wlow && r0 >= p.sinks)) continue;  // wave-uniform: nothing it sees
@@ -167,6 +171,22 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
         for (int kk = 0; kk < D / 16; ++kk)
           sc[kb] = Mma<bf16>::mma(*reinterpret_cast<const bf16x8*>(krow + lds_swz<CH>(kr, kk * 2 + g) * 16), qf[kk], sc[kb]);
       }
+    };
+    // V^T of rows 4 g + {0..3} and 8 + 4 g + {0..3} of 16, the order of the
+    // scores. Lane i of a 16-lane group addresses row i / 4 at channels
+    // 4 (i % 4) .. + 3 of the group's 16.
+    auto values = [&](int kb, int s2, int cb) {
+      const int k1 = kb * 32 + s2 * 16 + g * 4 + ((lane & 15) >> 2), ch = cb * 32 + (lane & 16) + 4 * (lane & 3);
+      auto addr = [&](int key) { return sv + key * RB + vtr_swz<CH>(key, ch / 8) * 16 + ((ch / 4) & 1) * 8; };
+      const auto a = __builtin_bit_cast(bf16x4, lds_read_tr16(addr(k1)));
+      const auto b = __builtin_bit_cast(bf16x4, lds_read_tr16(addr(k1 + 8)));
+      bf16x8 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = a[e];
+        v[e + 4] = b[e];
+      }
+      return v;
     };
     // scores scaled against `ref`; what is not seen counts for nothing
     auto against = [&](float ref) {
@@ -199,14 +219,19 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
     };
     float tsum = 0.0f;
     bool redo = !have_ref;
+    bf16x8 early[D / 32];  // of the first 16 rows, read while the exponentials are taken
     if (have_ref) {
       scores();
+#pragma unroll
+      for (int cb = 0; cb < D / 32; ++cb) early[cb] = values(0, 0, cb);
       against(mref);
       tsum = exponentiate();
       redo = __builtin_amdgcn_ballot_w64(!(lrun + tsum <= kSumLimit)) != 0;
     }
     if (redo) {  // wave-uniform: the first tile, a sum past the limit, or a lane's first row
       scores();
+#pragma unroll
+      for (int cb = 0; cb < D / 32; ++cb) early[cb] = values(0, 0, cb);
       against(0.0f);
       float mt = -INFINITY;
 #pragma unroll
@@ -241,24 +266,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(sc[kb][s2 * 8 + 2 * i], sc[kb][s2 * 8 + 2 * i + 1]);
         const bf16x8 pb = __builtin_bit_cast(bf16x8, w);
-        // rows 4 g + {0..3} and 8 + 4 g + {0..3} of these 16: the order of pb.
-        // Lane i of a 16-lane group addresses row i / 4 at channels 4 (i % 4)
-        // .. + 3 of the group's 16.
-        const int k1 = kb * 32 + s2 * 16 + g * 4 + ((lane & 15) >> 2);
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) {
-          const int ch = cb * 32 + (lane & 16) + 4 * (lane & 3);
-          auto addr = [&](int key) { return sv + key * RB + vtr_swz<CH>(key, ch / 8) * 16 + ((ch / 4) & 1) * 8; };
-          const auto a = __builtin_bit_cast(bf16x4, lds_read_tr16(addr(k1)));
-          const auto b = __builtin_bit_cast(bf16x4, lds_read_tr16(addr(k1 + 8)));
-          bf16x8 va;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            va[e] = a[e];
-            va[e + 4] = b[e];
-          }
-          o[cb] = Mma<bf16>::mma(va, pb, o[cb]);
-        }
+        for (int cb = 0; cb < D / 32; ++cb)
+          o[cb] = Mma<bf16>::mma(kb == 0 && s2 == 0 ? early[cb] : values(kb, s2, cb), pb, o[cb]);
       }
   }
 

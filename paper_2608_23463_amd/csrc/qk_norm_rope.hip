@@ -523,8 +523,6 @@ TurnParams turn_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, con
   return t;
 }
 
-constexpr int kTokensPerWave = 4;
-
 template <class F>
 hipError_t timed(const char* label, hipStream_t s, F&& f) {
   const bool tr = trace_on();
@@ -535,6 +533,9 @@ hipError_t timed(const char* label, hipStream_t s, F&& f) {
   return e;
 }
 
+// Tokens below which a wave takes one pass: 2,000 x (16 + 16) x 64 6.2 us (6.7
+// with a wave per token), an append of 500 tokens 5.3 (7.2), of 4,000 x (32 + 8
+// + 8) x 128 22.4 (20.2).
 constexpr int64_t kFewTokens = 2048;
 
 template <typename T, int D, bool PAIRS, bool APPEND>
@@ -547,9 +548,19 @@ hipError_t forward_on(QkParams p, int64_t n, const char* label, hipStream_t s) {
       const int64_t units = n * p.fparts.d;
       qk_few_kernel<T, D, PAIRS, APPEND><<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
     } else {
-      const int64_t units = (n + kTokensPerWave - 1) / kTokensPerWave;
-      qk_forward_kernel<T, D, PAIRS, kTokensPerWave, APPEND>
-          <<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
+      // One token per wave while its rows fill the passes to two thirds: its
+      // loads start earliest (65,536 x (16 + 4) x 128: 127 us, with four tokens
+      // 136). With few heads, whose passes would run part empty, four
+      // (100,000 x (4 + 1) x 64: 32 us, with one 76).
+      const int passes = (p.q.p ? (p.hq + RPP - 1) / RPP : 0) + (APPEND ? 2 : 1) * ((p.hk + RPP - 1) / RPP);
+      const int rows = (p.q.p ? p.hq : 0) + (APPEND ? 2 : 1) * p.hk;
+      const bool single = 2 * passes * RPP <= 3 * rows;
+      const int per = kWaves * (single ? 1 : 4);
+      const dim3 grid((unsigned)((n + per - 1) / per));
+      if (single)
+        qk_forward_kernel<T, D, PAIRS, 1, APPEND><<<grid, kThreads, 0, s>>>(p);
+      else
+        qk_forward_kernel<T, D, PAIRS, 4, APPEND><<<grid, kThreads, 0, s>>>(p);
     }
   });
 }
@@ -580,8 +591,8 @@ QkParams qk_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, const i
   return p;
 }
 
-constexpr int kBwdTokens = 4;      // tokens per wave and step of the backward
-constexpr int kBwdBlocks = 1024;   // workgroups at most (their gain sums are joined)
+constexpr int kBwdTokens = 2;    // tokens per wave and step of the backward
+constexpr int kBwdBlocks = 768;  // workgroups at most: three per CU, as their registers allow
 
 int bwd_blocks(int64_t n) {
   const int64_t per = (int64_t)kWaves * kBwdTokens;

@@ -275,10 +275,10 @@ def test_attend_prompts(gpu, name):
     t = int(cu[-1]) + pad
     q = draw(rng, (t, hq, d), dtype, 2)
     scale = 1 / np.sqrt(d)
-    for max_new in (max(new), 1, 4000):
+    for max_new, longest in ((max(new), max(lens)), (1, max(lens)), (4000, 64)):
         out = torch.full((t, hq, d), 7.0, dtype=torch_dtype(dtype), device="cuda")
         lse = torch.full((t, hq), 7.0, device="cuda")
-        p.cache.attend(laid_out(q, dtype, "heads"), max(lens), cu_tokens=torch.from_numpy(cu).cuda(), max_new=max_new,
+        p.cache.attend(laid_out(q, dtype, "heads"), longest, cu_tokens=torch.from_numpy(cu).cuda(), max_new=max_new,
                        window=window, sinks=sinks, out=out, lse=lse)
         torch.cuda.synchronize()
         check_attend(p, q, out, lse, cu, window, sinks, scale, (name, max_new), max_new)
