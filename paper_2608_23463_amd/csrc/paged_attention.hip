@@ -356,31 +356,41 @@ __global__ void __launch_bounds__(kThreads, (Tile<T, D>::kPerCu)) paged_attentio
   }
 }
 
-// Joins the slices of a (token, head) in a fixed order: a lane per four
-// channels, the streams of slices joined through LDS.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
-  constexpr int C4 = D / 4, NS = kThreads / C4;
-  __shared__ float so[NS][D];
-  __shared__ float sl[NS];
-  const int row = blockIdx.x, tok = row / p.hq, head = (row - tok * p.hq) % p.group;
+// The slices that hold a (token, head)'s partial results, 0 .. live - 1 of its
+// row; -1: a token behind the last sequence.
+__device__ __forceinline__ int live_slices(const PagedParams& p, int row) {
+  const int tok = row / p.hq, head = (row - tok * p.hq) % p.group;
   const int s0 = p.cu ? find_sequence(p.batch, [&](int c) { return p.cu[c]; }, tok) : tok;
   Sequence sq;
   sq.set(p, s0);
   const int x = (tok - sq.t0) * p.group + head;
-  if (sq.seq < 0 || x < 0 || x >= sq.cols) return;  // behind the last sequence
+  if (sq.seq < 0 || x < 0 || x >= sq.cols) return -1;
   const int x0 = x & -p.cols;  // its block's first column
   const Sight sight(p, sq, x0, min(sq.cols - x0, p.cols), p.tile_rows);
   const int per = sight.per_slice(p);
-  const int live = (sight.tiles + per - 1) / per;
+  return (sight.tiles + per - 1) / per;
+}
+
+// Joins the slices of a row in a fixed order, ROWS rows per workgroup: four of
+// few slices, a wave each, or one of many. A lane takes four channels; the
+// streams of slices are joined through LDS. (With a workgroup per row 78,000
+// rows of two slices took 150 us.)
+template <typename T, int D, int ROWS>
+__global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
+  constexpr int C4 = D / 4, NS = kThreads / ROWS / C4;  // streams of a row
+  __shared__ float so[ROWS][NS][D];
+  __shared__ float sl[ROWS][NS];
+  const int lane = threadIdx.x % kWave, at = threadIdx.x % (kThreads / ROWS), r = threadIdx.x / (kThreads / ROWS);
+  const int row = __builtin_amdgcn_readfirstlane((int)blockIdx.x * ROWS + r);
+  const int live = row < p.n_tokens * p.hq ? live_slices(p, row) : -1;
   const float2* ml = p.part_ml + (int64_t)row * p.slices;
   const float* po = p.part_o + (int64_t)row * p.slices * D;
   float top = -INFINITY;
-  for (int s = threadIdx.x % kWave; s < live; s += kWave) top = fmaxf(top, ml[s].x);
+  for (int s = lane; s < live; s += kWave) top = fmaxf(top, ml[s].x);
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
   const float ref = top == -INFINITY ? 0.0f : top;
-  const int c = (threadIdx.x % C4) * 4, st = threadIdx.x / C4;
+  const int c = (at % C4) * 4, st = at / C4;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   float l = 0.0f;
   for (int s = st; s < live; s += NS) {
@@ -389,16 +399,16 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
     l += f * x.y;
     acc += f * *reinterpret_cast<const f32x4*>(po + (int64_t)s * D + c);
   }
-  *reinterpret_cast<f32x4*>(&so[st][c]) = acc;
-  if (c == 0) sl[st] = l;
+  *reinterpret_cast<f32x4*>(&so[r][st][c]) = acc;
+  if (c == 0) sl[r][st] = l;
   __syncthreads();
-  if (st == 0) {
+  if (st == 0 && live >= 0) {
     l = 0.0f;
     acc = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      l += sl[s];
-      acc += *reinterpret_cast<const f32x4*>(&so[s][c]);
+      l += sl[r][s];
+      acc += *reinterpret_cast<const f32x4*>(&so[r][s][c]);
     }
     const float inv = l > 0.0f ? 1.0f / l : l;
     float res[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
@@ -406,6 +416,8 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
     if (p.lse && c == 0) p.lse[row] = (top + __log2f(l)) * 0.69314718055994530942f;
   }
 }
+
+constexpr int kFewSlices = 8;  // slices up to which a wave joins a row
 
 template <typename T, int D>
 hipError_t attention_on(const PagedParams& p, const PagedPlan& pl, hipStream_t s) {
@@ -421,7 +433,11 @@ hipError_t attention_on(const PagedParams& p, const PagedPlan& pl, hipStream_t s
   if (tr) trace_end(s);
   if (e != hipSuccess || p.slices == 1) return e;
   if (tr) trace_begin("paged_join", s);
-  paged_join_kernel<T, D><<<dim3((unsigned)(p.n_tokens * p.hq)), kThreads, 0, s>>>(p);
+  const unsigned rows = (unsigned)(p.n_tokens * p.hq);
+  if (p.slices <= kFewSlices)
+    paged_join_kernel<T, D, 4><<<dim3((rows + 3) / 4), kThreads, 0, s>>>(p);
+  else
+    paged_join_kernel<T, D, 1><<<dim3(rows), kThreads, 0, s>>>(p);
   e = hipGetLastError();
   if (tr) trace_end(s);
   return e;
@@ -450,11 +466,11 @@ PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragge
   // by themselves, cuts only even out sequences of different lengths, and short
   // slices cost more than that gives (48 sequences of up to 9,000 rows, 8 heads:
   // 180 us in 768 workgroups, 159 in slices of 32 tiles; 64 sequences of up to
-  // 1,000 rows, 16 heads: 33 us whole, 41 in slices of 16). A prompt's groups
-  // are compute bound: eight tiles at least.
+  // 1,000 rows, 16 heads: 33 us whole, 41 in slices of 16). A prompt's slices
+  // have four tiles at least.
   const bool filled = pl.groups >= 256;
   const int64_t want = pl.prompt || !filled ? 512 : 4096;
-  pl.min_tiles = pl.prompt || pl.groups < 32 ? 8 : filled ? 32 : 16;
+  pl.min_tiles = pl.prompt ? 4 : pl.groups < 32 ? 8 : filled ? 32 : 16;
   int64_t s = std::min<int64_t>((want + pl.groups - 1) / pl.groups, (tiles + pl.min_tiles - 1) / pl.min_tiles);
   s = std::max<int64_t>(1, std::min<int64_t>(s, kMaxSlices));
   pl.slices = (int)s;

@@ -28,7 +28,7 @@ constexpr int kTile = 64;
 constexpr int kColumns = 128;
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p) {
+__global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel(PagedParams p) {
   constexpr int RB = D * 2, CH = RB / 16;     // bytes and 16-byte chunks of a row
   constexpr int kTileBytes = kTile * RB, kStage = 2 * kTileBytes;
   constexpr int kLoads = kBlock * RB / 1024;  // 1 KB loads of a wave's 16 rows
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
     const char* sk = smem + (t & 1) * kStage;
     const char* sv = sk + kTileBytes;
     if (r0 > wlast || (r0 + kTile - 1 <= wlow && r0 >= p.sinks)) continue;  // wave-uniform: nothing it sees
-    const bool whole = gone == 0 && r0 + kTile - 1 <= wfirst && (r0 > whigh || r0 + kTile <= p.sinks) && wcols == 32;
+    const bool whole = gone == 0 && r0 + kTile - 1 <= wfirst && (r0 > whigh || r0 + kTile <= p.sinks);
     f32x16 sc[2];
     auto scores = [&]() {
 #pragma unroll
@@ -194,16 +194,24 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prompt_kernel(PagedParams p
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[kb][r] = fmaf(sc[kb][r], p.scale_log2, -ref);
-      if (!whole) {
+      if (whole) return;
+      if (gone == 0 && r0 >= p.sinks) {  // the window's edges alone: one unsigned comparison
+        const int past = row - r0;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int in = kb * 32 + acc_row(r, lane), j = r0 + in;
-            const bool seen = j <= row && (j > lo || j < p.sinks) && !((gone >> (in / kBlock)) & 1);
-            if (!seen) sc[kb][r] = -INFINITY;
-          }
+          for (int r = 0; r < 16; ++r)
+            if ((unsigned)(past - (kb * 32 + acc_row(r, lane))) >= (unsigned)p.window) sc[kb][r] = -INFINITY;
+        return;
       }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int in = kb * 32 + acc_row(r, lane), j = r0 + in;
+          const bool seen = j <= row && (j > lo || j < p.sinks) && !((gone >> (in / kBlock)) & 1);
+          if (!seen) sc[kb][r] = -INFINITY;
+        }
     };
     auto exponentiate = [&]() {
       float ls[4] = {0.0f, 0.0f, 0.0f, 0.0f};
