@@ -391,7 +391,7 @@ typedef struct {
 /* Norm and rotation in training.
  *  q, q_out [n_tokens, n_heads], k, k_out [n_tokens, n_kv_heads] rows
  *  positions int32 [n_axes, n_tokens] (device; NULL if rot_dim is 0)
- * n_tokens below 2^31; 0 does nothing. */
+ * n_tokens below 2^26 (here and in the append); 0 does nothing. */
 int proxy_qk_norm_rope_forward(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n_tokens,
                                const pf_rows* q, const pf_rows* k, const int32_t* positions,
                                const pf_rows* q_out, const pf_rows* k_out, void* stream);
@@ -471,7 +471,8 @@ int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, co
  *  given), aligned to 256; 0 when no sequence is cut, and for invalid sizes.
  *  Calls that may run at the same time, graphs' replays among them, need
  *  workspaces of their own.
- * n_tokens * n_heads below 2^31; n_tokens = 0 does nothing. The result does
+ * n_tokens * n_heads below 2^28, batch * n_kv_heads below 2^24; n_tokens = 0
+ * does nothing. The result does
  * not depend on where pages lie and is the same in every run. */
 size_t proxy_paged_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
                                   int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks);

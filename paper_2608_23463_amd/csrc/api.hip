@@ -518,7 +518,7 @@ static int check_heads(const pf_heads_config* cfg, const pf_heads_weights* w, in
   if (st != PF_OK) return fail(st, "invalid heads config: %s", why);
   if (!w) return fail(PF_ERR_INVALID_ARG, "weights struct is NULL");
   if (n < 0) return fail(PF_ERR_INVALID_ARG, "n_tokens must be >= 0");
-  if (n > INT32_MAX) return fail(PF_ERR_UNSUPPORTED, "n_tokens above 2^31 - 1");
+  if (n > kMaxTokens) return fail(PF_ERR_UNSUPPORTED, "n_tokens above %lld", (long long)kMaxTokens);
   if (d->norm && (!aligned16(w->gamma_q) || !aligned16(w->gamma_k)))
     return fail(PF_ERR_INVALID_ARG, "gains must be 16-byte aligned");
   if (d->rot && !w->freqs) return fail(PF_ERR_INVALID_ARG, "freqs is NULL");
@@ -557,7 +557,7 @@ int proxy_qk_norm_rope_forward(const pf_heads_config* cfg, const pf_heads_weight
 size_t proxy_qk_workspace_size(const pf_heads_config* cfg, int64_t n_tokens) {
   HeadsDims d;
   const char* why;
-  if (heads_dims(cfg, &d, &why) != PF_OK || n_tokens < 0 || n_tokens > INT32_MAX) return 0;
+  if (heads_dims(cfg, &d, &why) != PF_OK || n_tokens < 0 || n_tokens > kMaxTokens) return 0;
   return qk_backward_ws(d, n_tokens);
 }
 
@@ -694,8 +694,11 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
   if (window < 0 || sinks < 0) return fail(PF_ERR_INVALID_ARG, "window and sinks must be >= 0");
   if (!std::isfinite(scale)) return fail(PF_ERR_INVALID_ARG, "scale must be finite");
   if (n_tokens == 0) return PF_OK;
-  if (n_tokens > INT32_MAX / d.hq) return fail(PF_ERR_UNSUPPORTED, "n_tokens * n_heads above 2^31 - 1");
+  if (n_tokens > INT32_MAX / d.hq) return fail(PF_ERR_UNSUPPORTED, "n_tokens * n_heads above 2^28");
   const int64_t n = n_tokens;
+  const PagedPlan pl = paged_plan(d, c.batch, n, cu_tokens != nullptr, max_new, max_kv_len, window, sinks);
+  if (pl.groups > kMaxGroups / pl.slices)
+    return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes: n_tokens * n_heads must stay below 2^28");
   if ((st = check_rows("q", q, n, d.hq, d, false)) != PF_OK) return st;
   if (!out) return fail(PF_ERR_INVALID_ARG, "out is NULL");
   if (!aligned16(out)) return fail(PF_ERR_INVALID_ARG, "out must be 16-byte aligned");
@@ -703,8 +706,6 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
   const size_t out_bytes = (size_t)n * d.hq * d.d * d.esize;
   if (overlaps(out, out_bytes, q->p, rows_bytes(*q, n, d.hq, d)))
     return fail(PF_ERR_INVALID_ARG, "out must not overlap q");
-  const PagedPlan pl = paged_plan(d, c.batch, n, cu_tokens != nullptr, max_new, max_kv_len, window, sinks);
-  if (pl.groups > INT32_MAX / pl.slices) return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes");
   if (pl.bytes && (!workspace || ws_bytes < pl.bytes))
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", pl.bytes, workspace ? ws_bytes : 0);
   if (!aligned16(workspace)) return fail(PF_ERR_INVALID_ARG, "workspace must be 16-byte aligned");

@@ -46,6 +46,28 @@ struct PagedDims {
   int batch;
 };
 
+// A launch has fewer than 2^32 threads in a dimension: workgroups of 256 at most.
+constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 1;
+// Tokens of a call: four per workgroup at least.
+constexpr int64_t kMaxTokens = 4 * kMaxGroups;
+
+// The largest s < count with at(s) <= x, where at rises and at(0) <= x: the
+// wave probes 64 places at a time, each time within the run that is left. Of
+// boundaries that do not rise it is some s in range.
+template <class F>
+__device__ __forceinline__ int find_run(int count, F&& at, int64_t x) {
+  const int lane = (int)(threadIdx.x & (kWave - 1));
+  int s = 0;
+  for (int n = count; n > 1;) {
+    const int step = (n + kWave - 1) / kWave, c = lane * step;
+    const bool below = c < n && at(s + (c < n ? c : 0)) <= x;
+    const int k = max((int)__popcll(__ballot(below)) - 1, 0);
+    s += k * step;
+    n = min(step, n - k * step);
+  }
+  return __builtin_amdgcn_readfirstlane(s);
+}
+
 int heads_dims(const pf_heads_config* c, HeadsDims* d, const char** why);
 
 // Forward: q -> q_out, k -> k_out. n_tokens rows, positions [n_axes, n_tokens].

@@ -20,7 +20,7 @@ struct PagedParams {
   int n_pages, page_size, max_pages, batch, n_tokens;
   FastDiv page_blocks;  // blocks per page
   int hq, hk, group;
-  FastDiv fgroup, fhk, fslices;
+  FastDiv fgroup, fhk, fslices, fblocks;  // fblocks: blocks of a sequence without cu
   int cols, tile_rows;  // queries of a workgroup, rows of a tile (both powers of two)
   int slices, min_tiles;
   int window, sinks;    // window: INT32_MAX without one
@@ -65,33 +65,27 @@ template <int COLS>
 __device__ __forceinline__ int first_block(const PagedParams& p, int s) {
   return p.cu ? (int)((int64_t)p.cu[s] * p.group / COLS) + s : s * ((p.group + COLS - 1) / COLS);
 }
+template <int COLS>
+__device__ __forceinline__ int sequence_of_block(const PagedParams& p, int blk) {
+  return p.cu ? find_run(p.batch, [&](int c) { return first_block<COLS>(p, c); }, blk) : p.fblocks.div(blk);
+}
 // Their number (n_tokens < 0: one token of every sequence).
 inline int64_t col_blocks(int cols, int group, int64_t n_tokens, int batch) {
   return n_tokens < 0 ? (int64_t)batch * ((group + cols - 1) / cols) : n_tokens * group / cols + batch;
 }
 
-// The largest s < batch with at(s) <= x, counted by the wave, 64 at a time
-// (at rises with s, at(0) <= x).
-template <class F>
-__device__ __forceinline__ int find_sequence(int batch, F&& at, int64_t x) {
-  int s = 0;
-  for (int i = 1; i < batch; i += kWave) {
-    const int c = i + (int)(threadIdx.x & (kWave - 1));
-    s += __popcll(__ballot(c < batch && at(c < batch ? c : 0) <= x));
-  }
-  return __builtin_amdgcn_readfirstlane(s);
-}
-
 // The rows that a block of columns sees, as a list of tiles: those of the
 // first rows, then those of the windows.
 struct Sight {
-  int first, last;  // rows of its first and last token (last = -1: it sees none)
+  int first, top;   // rows of its first and last token
+  int last;         // the last row that it sees: top, or the table's end (-1: none)
   int head_tiles;   // tiles that hold the first rows
   int gap;          // added to later tile numbers
   int tiles;
   __device__ __forceinline__ Sight(const PagedParams& p, const Sequence& sq, int x0, int cols, int tile_rows) {
     first = max(sq.row0 + p.fgroup.div(x0), 0);
-    last = max(min(sq.row0 + p.fgroup.div(x0 + cols - 1), sq.most - 1), -1);
+    top = max(sq.row0 + p.fgroup.div(x0 + cols - 1), -1);
+    last = min(top, sq.most - 1);
     const int lo = max(first - p.window + 1, 0), n = last + 1;
     head_tiles = (min(p.sinks, lo) + tile_rows - 1) / tile_rows;
     gap = max(lo / tile_rows - head_tiles, 0);

@@ -204,17 +204,6 @@ __device__ __forceinline__ int position_of(const TurnParams& t, int64_t tok, int
   return t.positions[(int64_t)axis * t.n + tok];
 }
 
-// Sequence of a token of a ragged batch: the number of boundaries cu[1..B]
-// at or before it, counted by the wave, 64 at a time. B: behind the last one.
-__device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int64_t tok) {
-  int s = 0;
-  for (int i = 0; i < batch; i += kWave) {
-    const int at = i + (int)(threadIdx.x & (kWave - 1));
-    s += __popcll(__ballot(at < batch && cu[at + 1] <= tok));
-  }
-  return s;
-}
-
 // One tensor's rows of a launch: which = 0 queries, 1 keys, 2 values (append:
 // copied as they are).
 struct Tensor {
@@ -260,7 +249,7 @@ __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, floa
 // behind the last sequence or without a place; `at` is its row of the sequence,
 // kv_len - new + i for the i-th new token.
 __device__ __forceinline__ int64_t place_of(const QkParams& p, int64_t tok, int* at) {
-  const int s = p.cu ? sequence_of(p.cu, p.batch, tok) : (int)tok;
+  const int s = p.cu ? find_run(p.batch + 1, [&](int c) { return p.cu[c]; }, tok) : (int)tok;
   *at = 0;
   if (s >= p.batch) return -1;
   const int64_t pos = p.cu ? (int64_t)p.kv_len[s] - p.cu[s + 1] + tok : (int64_t)p.kv_len[s] - 1;

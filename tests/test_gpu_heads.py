@@ -134,6 +134,68 @@ def test_backward(gpu, name):
             assert got[2 + i] is None
 
 
+@pytest.mark.parametrize("name", ["T3_h1x128_fp32_pairs", "T130_h17x64_fp32_uneven_axes", "T33_norm_only"])
+def test_backward_against_differences(gpu, name):
+    """The backward's derivative along a direction against a central difference
+    of the forward's results. The difference's own error is its distance in
+    float64 (the oracle's difference against its derivative) and the forward's
+    roundings (33 E m per element, twice) over the step."""
+    import torch
+    B, case = gpu, CASES[name]
+    t, hq, hk, d, dtype, norm, rot, pairs, axes, layout = case
+    a = qk_inputs(B, case, 3)
+    rng = np.random.default_rng(4)
+    h = 2.0 ** -7
+    along = {x: draw(rng, a[x].shape, dtype, float(np.abs(a[x]).mean())) for x in ("q", "k")}
+    dq, dk, _, _ = B.qk_norm_rope_backward(a["cfg"], a["w"], dev(a["q"], dtype), dev(a["k"], dtype), a["pos"],
+                                           dev(a["dq"], dtype), dev(a["dk"], dtype))
+    ends = []
+    for sign in (1, -1):
+        at = [(a[x] + np.float32(sign * h) * along[x]).astype(np.float32) for x in ("q", "k")]
+        out = B.qk_norm_rope_forward(a["cfg"], a["w"], dev(at[0], dtype), dev(at[1], dtype), a["pos"])
+        torch.cuda.synchronize()
+        ends.append([(at[i].astype(np.float64), host(out[i])) for i in range(2)])
+    for i, (x, dy, got) in enumerate((("q", a["dq"], host(dq)), ("k", a["dk"], host(dk)))):
+        g = a["g"][i]
+        exact = [O.norm_rope(e[i][0], g, 1e-5, norm, a["ang"], rot, pairs) for e in ends]
+        quotient = ((ends[0][i][1] - ends[1][i][1]) * dy).sum() / (2 * h)
+        ref = ((exact[0][0] - exact[1][0]) * dy).sum() / (2 * h)
+        step = (ends[0][i][0] - ends[1][i][0]) / (2 * h)  # the direction as fp32 took it
+        dx, _, mag, _ = O.norm_rope_backward(a[x], g, 1e-5, norm, a["ang"], rot, pairs, dy)
+        noise = sum((33 * E * e[1] * np.abs(dy)).sum() for e in exact) / (2 * h)
+        tol = noise + abs(ref - (dx * step).sum()) + ((E * np.abs(dx) + 64 * E * mag) * np.abs(step)).sum()
+        assert abs(quotient - (got * step).sum()) <= tol, (name, x, quotient, (got * step).sum(), tol)
+        assert tol < 0.05 * np.sqrt((dx ** 2).sum() * (step ** 2).sum())  # the comparison says something
+
+
+def test_training_calls_in_a_graph(gpu):
+    """Forward and backward captured together and replayed on new inputs, an
+    eager call of the same buffers between replays."""
+    import torch
+    B, case = gpu, CASES["T67_h12_4x128_video"]
+    a = qk_inputs(B, case, 5)
+    dt = case[4]
+    q, k, dq, dk = (dev(a[x], dt) for x in ("q", "k", "dq", "dk"))
+
+    def both():
+        out = B.qk_norm_rope_forward(a["cfg"], a["w"], q, k, a["pos"])
+        return (*out, *B.qk_norm_rope_backward(a["cfg"], a["w"], q, k, a["pos"], dq, dk))
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for i in range(4):
+        for x in (q, k, dq, dk):
+            x.copy_(torch.randn_like(x))
+        graph.replay()
+        torch.cuda.synchronize()
+        seen = [x.clone() for x in got]
+        for x, y in zip(seen, both()):
+            assert torch.equal(x, y)
+
+
 def test_no_tokens_and_missing_gains(gpu):
     import torch
     B = gpu
@@ -283,6 +345,67 @@ def test_attend_prompts(gpu, name):
         torch.cuda.synchronize()
         check_attend(p, q, out, lse, cu, window, sinks, scale, (name, max_new), max_new)
         assert (out[cu[-1]:] == 7).all() and (lse[cu[-1]:] == 7).all()
+
+
+def test_thousands_of_sequences(gpu):
+    """5,000 sequences in one call, most of them without a new token."""
+    import torch
+    rng = np.random.default_rng(13)
+    nb = 5000
+    new = [0] * nb
+    for i in (0, 63, 64, 65, 100, 2500, 4095, 4096, 4998):
+        new[i] = int(rng.integers(1, 40))
+    lens = [n + int(rng.integers(0, 20)) if n else 0 for n in new]
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    t = int(cu[-1]) + 2
+    cud = torch.from_numpy(cu).cuda()
+    p = Paged(gpu, rng, 2, 1, 64, "bf16", 16, lens, lens)
+    q, k = draw(rng, (t, 2, 64), "bf16"), draw(rng, (t, 1, 64), "bf16")
+    for max_new in (40, 1):
+        out = torch.full((t, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        p.cache.attend(dev(q, "bf16"), max(lens), cu_tokens=cud, max_new=max_new, out=out)
+        torch.cuda.synchronize()
+        check_attend(p, q, out, None, cu, 0, 0, 64 ** -0.5, max_new, max_new)
+        assert (out[-2:] == 7).all()
+    p.cache.append(dev(k, "bf16"), dev(k, "bf16"), cu_tokens=cud)
+    torch.cuda.synchronize()
+    kd = host(p.vd)
+    for i, (s, row) in enumerate(O.token_rows(lens, cu)):
+        pg, sl = O.place(p.table[s], row, 16, p.n_pages)
+        assert np.array_equal(kd[pg, :, sl], k[i])
+
+
+@pytest.mark.parametrize("held", [64, 48, 16])
+def test_lengths_past_the_table(gpu, held):
+    """kv_len beyond what the table holds, whether or not that ends a tile: its
+    rows are seen, the others are not, and nothing is written past it."""
+    import torch
+    rng = np.random.default_rng(14)
+    p = Paged(gpu, rng, 4, 2, 64, "bf16", 16, [held, 30], [held, 30], extra_pages=0)
+    p.lens = [held + 50, 30]
+    p.ld.copy_(torch.tensor(p.lens, dtype=torch.int32))
+    q = draw(rng, (2, 4, 64), "bf16")
+    for window, sinks in ((0, 0), (60, 0), (20, 3)):
+        out = p.cache.attend(dev(q, "bf16"), 64, window=window, sinks=sinks)
+        torch.cuda.synchronize()
+        check_attend(p, q, out, None, None, window, sinks, 64 ** -0.5, window)
+    before = p.kd.clone()
+    kv = dev(draw(rng, (2, 2, 64), "bf16"), "bf16")
+    p.cache.append(kv, kv)
+    torch.cuda.synchronize()
+    assert (p.kd.view(torch.int16) != before.view(torch.int16)).any(-1).any(1).nonzero().tolist() == [[p.table[1, 1], 13]]
+    p.lens = [held + 20, 30]
+    p.ld.copy_(torch.tensor(p.lens, dtype=torch.int32))
+    p.kd.copy_(dev(p.k, "bf16"))
+    p.vd.copy_(dev(p.v, "bf16"))
+    new = np.array([0, 40, 40], np.int32)
+    for max_new in (40, 1):
+        for window, sinks in ((0, 0), (30, 2)):
+            q = draw(rng, (40, 4, 64), "bf16")
+            out = p.cache.attend(dev(q, "bf16"), 64, cu_tokens=torch.from_numpy(new).cuda(), max_new=max_new,
+                                 window=window, sinks=sinks)
+            torch.cuda.synchronize()
+            check_attend(p, q, out, None, new, window, sinks, 64 ** -0.5, (max_new, window), max_new)
 
 
 def test_pages_that_are_none(gpu):

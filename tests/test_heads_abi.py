@@ -118,7 +118,8 @@ def test_pointers_and_counts():
     refused(forward(pos=None))
     refused(forward(pos=P + 2))
     refused(forward(n=-1))
-    refused(forward(n=1 << 31), B.PF_ERR_UNSUPPORTED)
+    refused(forward(n=1 << 26), B.PF_ERR_UNSUPPORTED)
+    refused(backward(n=1 << 26), B.PF_ERR_UNSUPPORTED)
     refused(backward(pos=None))
     refused(backward(gq=5 * P + 2))
     refused(backward(ws=None), B.PF_ERR_WORKSPACE)
@@ -174,7 +175,8 @@ def test_paged_arguments():
     refused(append(cu=P + 2))
     refused(attend(cu=P + 2))
     refused(append(pos=P + 2))
-    refused(append(n=1 << 31, cu=P), B.PF_ERR_UNSUPPORTED)
+    refused(append(n=1 << 26, cu=P), B.PF_ERR_UNSUPPORTED)
+    refused(attend(n=1 << 25, cu=P), B.PF_ERR_UNSUPPORTED)
     refused(attend(n=1 << 29, cu=P), B.PF_ERR_UNSUPPORTED)
     for bad in (dict(max_new=0), dict(max_kv=0), dict(window=-1), dict(sinks=-1), dict(scale=float("nan")),
                 dict(scale=float("inf")), dict(out=None), dict(out=5 * P + 8), dict(lse=P + 2), dict(ws=6 * P + 4)):
