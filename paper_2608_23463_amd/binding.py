@@ -621,11 +621,13 @@ def _want(name, t, dtype, device, shape, contiguous=True):
 
 def _rows(cfg, name, t, n, heads, device) -> PfRows:
     """The rows of a tensor [tokens, heads, head_dim]; only a row itself must be contiguous."""
-    p = _want(name, t, _heads_dtype(cfg), device, (n, heads, cfg.head_dim), contiguous=False)
+    dtype, shape = _heads_dtype(cfg), (n, heads, cfg.head_dim)
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        _want(name, t, dtype, device, shape, contiguous=False)  # raises
     ts, hs, es = t.stride()
     if es != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    return PfRows(p, ts if n > 1 else 0, hs if heads > 1 else 0)
+    return PfRows(t.data_ptr(), ts if n > 1 else 0, hs if heads > 1 else 0)
 
 
 def _heads_weights(cfg, weights: Dict[str, object], device) -> PfHeadsWeights:

@@ -82,9 +82,9 @@ hipError_t launch_qk_backward(const HeadsDims& d, const HeadsWeights& w, int64_t
                               const int32_t* positions, const Rows& dq_out, const Rows& dk_out, const Rows& dq,
                               const Rows& dk, float* dgamma_q, float* dgamma_k, float* ws, hipStream_t s);
 
-// Attention over the cache: how its rows are cut. The rows that a block of
-// queries sees are cut into at most `slices` runs of at least `min_tiles`
-// tiles, by its own length.
+// Attention over the cache: how its rows are cut. The tiles that a block of
+// queries sees are cut into at most `slices` runs of at least `min_tiles`, by
+// its own length.
 struct PagedPlan {
   bool prompt;       // paged_prompt_kernel, or the one for single tokens
   int cols, tile_rows;

@@ -22,7 +22,8 @@ struct PagedParams {
   int hq, hk, group;
   FastDiv fgroup, fhk, fslices, fblocks;  // fblocks: blocks of a sequence without cu
   int cols, tile_rows;  // queries of a workgroup, rows of a tile (both powers of two)
-  int slices, min_tiles;
+  int slices;           // at most
+  FastDiv fmin_tiles;   // least tiles of a slice
   int window, sinks;    // window: INT32_MAX without one
   float scale_log2;
   void* out;
@@ -92,9 +93,10 @@ struct Sight {
     tiles = max((n + tile_rows - 1) / tile_rows - gap, 0);
   }
   __device__ __forceinline__ int tile(int i) const { return i < head_tiles ? i : i + gap; }
+  // As many slices as leave each min_tiles, all of the same size but the last.
   __device__ __forceinline__ int per_slice(const PagedParams& p) const {
-    const int even = (tiles + p.slices - 1) / p.slices;
-    return even > p.min_tiles ? even : p.min_tiles;
+    const int n = max(min(p.fmin_tiles.div(tiles), p.slices), 1);
+    return max((tiles + n - 1) / n, 1);
   }
 };
 

@@ -180,13 +180,17 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, (Tile<T, D>::kPerCu)) paged_attention_kernel(PagedParams p) {
   typedef Tile<T, D> Tl;
   constexpr int NB = Tl::NB, TR = NB * kBlock;
-  __shared__ float so[kWaves][kCols][D];
+  __shared__ __attribute__((aligned(16))) float so[kWaves][kCols][D + 4];  // columns four banks apart
   __shared__ float sm[kWaves][kCols], sl[kWaves][kCols];
 
-  // slices fastest, then K/V heads, then blocks of columns
-  int id = (int)blockIdx.x;
-  int up = p.fslices.div(id);
-  const int slice = id - up * p.slices;
+  // Slices fastest, then K/V heads, then blocks of columns; every group begins
+  // at another slice. Workgroups go to the XCDs in turn, and short sequences
+  // fill their first slices only: with eight slices in order most of the rows
+  // would go to the first XCDs (48 sequences of up to 9,000 rows: 207 us, and 167
+  // so).
+  const int id = (int)blockIdx.x, up = p.fslices.div(id);
+  int slice = id - up * p.slices + up - p.fslices.div(up) * p.slices;
+  slice -= slice >= p.slices ? p.slices : 0;
   const int blk = p.fhk.div(up), hk = up - blk * p.hk;
   const int s = sequence_of_block<kCols>(p, blk);
   Sequence sq;
@@ -468,17 +472,18 @@ PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragge
   const int64_t tiles = std::max<int64_t>(1, (rows + pl.tile_rows - 1) / pl.tile_rows);
   pl.groups = col_blocks(pl.cols, d.hq / d.hk, ragged ? n_tokens : -1, batch) * d.hk;
   // Few groups: two workgroups per CU, if that leaves each enough tiles (fewer
-  // and longer slices stream better: 8 heads over 1M rows take 702 us in 512
-  // workgroups, 729 in 2,048 and 760 in 4,096). Where the groups fill the chip
-  // by themselves, cuts only even out sequences of different lengths, and short
-  // slices cost more than that gives (48 sequences of up to 9,000 rows, 8 heads:
-  // 180 us in 768 workgroups, 159 in slices of 32 tiles; 64 sequences of up to
-  // 1,000 rows, 16 heads: 33 us whole, 41 in slices of 16). A prompt's slices
-  // have four tiles at least.
+  // and longer slices stream better: 8 heads over 1M rows take 700 us in 512
+  // workgroups, 729 in 2,048 and 760 in 4,096; 16 heads over 1,000 rows 9.2 us
+  // in slices of 8 tiles, 10.5 of 16, 8.8 of 4, which costs calls of few rows a
+  // join). Where the groups fill the chip by themselves, cuts only even out
+  // sequences of different lengths, and short slices cost more than that gives:
+  // 48 sequences of up to 9,000 rows, 8 heads, 180 us in 768 workgroups, 158 in
+  // slices of 48 tiles, 153 of 24, and all of 4,100 rows 143, 143 and 151; 64
+  // sequences of up to 1,000 rows, 16 heads, 32 us whole, 47 in slices of 16.
   const bool filled = pl.groups >= 256;
   const int64_t want = pl.prompt || !filled ? 512 : 4096;
-  pl.min_tiles = pl.prompt ? 4 : pl.groups < 32 ? 8 : filled ? 32 : 16;
-  int64_t s = std::min<int64_t>((want + pl.groups - 1) / pl.groups, (tiles + pl.min_tiles - 1) / pl.min_tiles);
+  pl.min_tiles = pl.prompt ? 4 : pl.groups < 32 ? 8 : filled ? 48 : 16;
+  int64_t s = std::min<int64_t>((want + pl.groups - 1) / pl.groups, tiles / pl.min_tiles);
   s = std::max<int64_t>(1, std::min<int64_t>(s, kMaxSlices));
   pl.slices = (int)s;
   pl.bytes = s == 1 ? 0 : (size_t)n_tokens * d.hq * s * (d.d * sizeof(float) + sizeof(float2));
@@ -510,7 +515,7 @@ hipError_t launch_paged_attention(const HeadsDims& d, const PagedDims& c, const 
   p.cols = pl.cols;
   p.tile_rows = pl.tile_rows;
   p.slices = pl.slices;
-  p.min_tiles = pl.min_tiles;
+  p.fmin_tiles = FastDiv(pl.min_tiles);
   p.fslices = FastDiv(pl.slices);
   p.fhk = FastDiv(d.hk);
   p.fgroup = FastDiv(p.group);
