@@ -90,7 +90,8 @@ struct Sight {
     const int lo = max(first - p.window + 1, 0), n = last + 1;
     head_tiles = (min(p.sinks, lo) + tile_rows - 1) / tile_rows;
     gap = max(lo / tile_rows - head_tiles, 0);
-    tiles = max((n + tile_rows - 1) / tile_rows - gap, 0);
+    const int all = (n + tile_rows - 1) / tile_rows;  // (the windows may lie past the table's end)
+    tiles = min(head_tiles, all) + max(all - head_tiles - gap, 0);
   }
   __device__ __forceinline__ int tile(int i) const { return i < head_tiles ? i : i + gap; }
   // As many slices as leave each min_tiles, all of the same size but the last.

@@ -478,11 +478,11 @@ PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragge
   // join). Where the groups fill the chip by themselves, cuts only even out
   // sequences of different lengths, and short slices cost more than that gives:
   // 48 sequences of up to 9,000 rows, 8 heads, 180 us in 768 workgroups, 158 in
-  // slices of 48 tiles, 153 of 24, and all of 4,100 rows 143, 143 and 151; 64
+  // slices of 48 tiles, 153 of 24 (and all of 4,100 rows 143, 143 and 151); 64
   // sequences of up to 1,000 rows, 16 heads, 32 us whole, 47 in slices of 16.
   const bool filled = pl.groups >= 256;
   const int64_t want = pl.prompt || !filled ? 512 : 4096;
-  pl.min_tiles = pl.prompt ? 4 : pl.groups < 32 ? 8 : filled ? 48 : 16;
+  pl.min_tiles = pl.prompt ? 4 : pl.groups < 32 ? 8 : filled ? 24 : 16;
   int64_t s = std::min<int64_t>((want + pl.groups - 1) / pl.groups, tiles / pl.min_tiles);
   s = std::max<int64_t>(1, std::min<int64_t>(s, kMaxSlices));
   pl.slices = (int)s;

@@ -94,7 +94,7 @@ struct TurnParams {
   const double* freqs;
   const int32_t* positions;  // [n_axes, n] or NULL (append: by the cache)
   int64_t n;
-  int rot, n_axes;
+  int rot;
   int axis_end[PF_MAX_AXES];
 };
 
@@ -507,7 +507,6 @@ TurnParams turn_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, con
   t.positions = positions;
   t.n = n;
   t.rot = d.rot;
-  t.n_axes = d.n_axes;
   for (int i = 0; i < PF_MAX_AXES; ++i) t.axis_end[i] = d.axis_end[i];
   return t;
 }

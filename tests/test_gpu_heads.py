@@ -375,14 +375,15 @@ def test_thousands_of_sequences(gpu):
         assert np.array_equal(kd[pg, :, sl], k[i])
 
 
+@pytest.mark.parametrize("past", [50, 700])
 @pytest.mark.parametrize("held", [64, 48, 16])
-def test_lengths_past_the_table(gpu, held):
+def test_lengths_past_the_table(gpu, held, past):
     """kv_len beyond what the table holds, whether or not that ends a tile: its
     rows are seen, the others are not, and nothing is written past it."""
     import torch
     rng = np.random.default_rng(14)
     p = Paged(gpu, rng, 4, 2, 64, "bf16", 16, [held, 30], [held, 30], extra_pages=0)
-    p.lens = [held + 50, 30]
+    p.lens = [held + past, 30]
     p.ld.copy_(torch.tensor(p.lens, dtype=torch.int32))
     q = draw(rng, (2, 4, 64), "bf16")
     for window, sinks in ((0, 0), (60, 0), (20, 3)):
@@ -394,7 +395,7 @@ def test_lengths_past_the_table(gpu, held):
     p.cache.append(kv, kv)
     torch.cuda.synchronize()
     assert (p.kd.view(torch.int16) != before.view(torch.int16)).any(-1).any(1).nonzero().tolist() == [[p.table[1, 1], 13]]
-    p.lens = [held + 20, 30]
+    p.lens = [held + past - 30, 30]
     p.ld.copy_(torch.tensor(p.lens, dtype=torch.int32))
     p.kd.copy_(dev(p.k, "bf16"))
     p.vd.copy_(dev(p.v, "bf16"))
