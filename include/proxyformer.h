@@ -417,7 +417,8 @@ int proxy_qk_norm_rope_backward(const pf_heads_config* cfg, const pf_heads_weigh
  *  page_table int32 [batch, max_pages]: page i of sequence b holds its rows
  *  i * page_size ..; max_pages * page_size at most 2^31 - 65536. Entries past
  *  a sequence's length are not read; an entry outside 0..n_pages-1 stands for
- *  no page: nothing is written there, and its rows are not seen.
+ *  no page: nothing is written there, and its rows are not seen. Sequences may
+ *  share pages (of a common beginning) that no append writes.
  *  kv_len int32 [batch]: rows of every sequence, those of the tokens being
  *  appended among them (one array serves a step's append and its attention in
  *  every layer). 0 or less: an empty slot.

@@ -789,8 +789,10 @@ class PagedCache:
         `window` and the first `sinks`. max_kv_len, max_new: most rows and new
         tokens of a sequence, to lay the launch out for (max_new: 1 without
         cu_tokens, T with it unless given). scale: 1 / sqrt(head_dim) unless
-        given. lse: an fp32 [T, n_heads] tensor for the log-sums. Returns out;
-        rows of tokens behind the last sequence are left alone."""
+        given. lse: an fp32 [T, n_heads] tensor for the log-sums. workspace: a
+        byte tensor that no call running at the same time uses (allocated
+        unless given). Returns out; rows of tokens behind the last sequence are
+        left alone."""
         import torch
         cfg, dev, n = self.cfg, self.device, q.shape[0]
         ctx = _elsewhere(dev, stream)

@@ -246,12 +246,12 @@ __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, floa
 }
 
 // Where a token of an append goes: its row (head 0) in the pages, or -1 for one
-// behind the last sequence or without a place; `at` is its row of the sequence,
-// kv_len - new + i for the i-th new token.
+// of no sequence or without a place; `at` is its row of the sequence, kv_len -
+// new + i for the i-th new token.
 __device__ __forceinline__ int64_t place_of(const QkParams& p, int64_t tok, int* at) {
   const int s = p.cu ? find_run(p.batch + 1, [&](int c) { return p.cu[c]; }, tok) : (int)tok;
   *at = 0;
-  if (s >= p.batch) return -1;
+  if (s >= p.batch || (p.cu && tok < p.cu[s])) return -1;
   const int64_t pos = p.cu ? (int64_t)p.kv_len[s] - p.cu[s + 1] + tok : (int64_t)p.kv_len[s] - 1;
   if (pos < 0 || pos >= (int64_t)p.max_pages * p.page_size) return -1;
   *at = (int)pos;
