@@ -652,6 +652,17 @@ def _positions(cfg, positions, n, device):
     return _want("positions", positions, torch.int32, device, (cfg.n_axes, n))
 
 
+def _workspace(t, device):
+    """Data pointer and bytes of a call's workspace (None, 0 without one)."""
+    if t is None:
+        return None, 0
+    if t.device != device:
+        raise ValueError(f"workspace must be on the call's GPU {device}, got {t.device}")
+    if not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _elsewhere(device, stream):
     """None where a call on `device` with `stream` (None: the current one) can
     go out as it is; else the context that makes that GPU and stream current,
@@ -724,7 +735,7 @@ def qk_norm_rope_backward(cfg: PfHeadsConfig, weights: Dict[str, object], q, k, 
         gq, gk = _empty((2, cfg.head_dim), torch.float32, dev).unbind()
         if workspace is None:
             workspace = _bytes(int(lib.proxy_qk_workspace_size(cfg, n)), dev)
-        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        ws, ws_bytes = _workspace(workspace, dev)
     _check(lib.proxy_qk_norm_rope_backward(cfg, w, n, rq, rk, at, ro, rp, da, db, _ptr(gq), _ptr(gk), ws, ws_bytes,
                                            _current(dev)))
     return dq, dk, gq, gk
@@ -812,9 +823,7 @@ class PagedCache:
         if workspace is None:
             need = lib.proxy_paged_workspace_size(cfg, self.batch, n, cu is not None, max_new, max_kv_len, window, sinks)
             workspace = _bytes(need, dev) if need else None
-        ws, ws_bytes = None, 0
-        if workspace is not None:
-            ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        ws, ws_bytes = _workspace(workspace, dev)
         _check(lib.proxy_paged_attention(cfg, self.state, n, cu, rq, max_new, max_kv_len, window, sinks,
                                          cfg.head_dim ** -0.5 if scale is None else scale, to, tl, ws, ws_bytes,
                                          _current(dev)))

@@ -206,6 +206,17 @@ def test_binding_refuses_what_is_not_on_a_gpu():
                      torch.zeros(3, dtype=torch.int32))
 
 
+def test_binding_refuses_other_workspaces():
+    import torch
+    here = torch.device("meta")
+    ws = torch.empty(64, dtype=torch.uint8, device="meta")
+    assert B._workspace(ws, here)[1] == 64 and B._workspace(ws.view(torch.float32), here)[1] == 64
+    assert B._workspace(None, here) == (None, 0)
+    for bad in (torch.empty(64, dtype=torch.uint8), ws[::2]):  # elsewhere; with gaps that are not the caller's to give
+        with pytest.raises(ValueError):
+            B._workspace(bad, here)
+
+
 def test_rope_freqs():
     import torch
     f = B.rope_freqs(cfg(), device="cpu")
