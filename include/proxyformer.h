@@ -402,7 +402,8 @@ int proxy_qk_norm_rope_forward(const pf_heads_config* cfg, const pf_heads_weight
  * heads in a fixed order (NULL: not computed; with PF_NORM_NONE not written).
  * dq and dk may be dq_out's and dk_out's rows. n_tokens = 0 writes zero gain
  * gradients. workspace: proxy_qk_workspace_size bytes (0 without a norm, or
- * for an invalid config). */
+ * for an invalid config). It and the gain gradients overlap no other buffer of
+ * the call. */
 size_t proxy_qk_workspace_size(const pf_heads_config* cfg, int64_t n_tokens);
 int proxy_qk_norm_rope_backward(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n_tokens,
                                 const pf_rows* q, const pf_rows* k, const int32_t* positions,
@@ -457,7 +458,7 @@ int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, co
  * is r (as the append numbers them) sees the rows up to r: all of them, or
  * with window > 0 the last `window` and the first `sinks` (ignored where
  * window is 0). q [n_tokens, n_heads] rows, as the append gives them; out
- * [n_tokens, n_heads, head_dim] contiguous, not overlapping q; lse fp32
+ * [n_tokens, n_heads, head_dim] contiguous; lse fp32
  * [n_tokens, n_heads] or NULL: log of the sum of exp(scale * q.k), to join the
  * result with another attention's. A token that sees nothing (an empty slot):
  * out is zero and lse -inf. Tokens behind the last sequence: out and lse are
@@ -472,6 +473,7 @@ int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, co
  *  given), aligned to 256; 0 when no sequence is cut, and for invalid sizes.
  *  Calls that may run at the same time, graphs' replays among them, need
  *  workspaces of their own.
+ *  out, lse and workspace overlap neither each other nor what the call reads.
  * n_tokens * n_heads below 2^28, batch * n_kv_heads below 2^24; n_tokens = 0
  * does nothing. The result does
  * not depend on where pages lie and is the same in every run. */

@@ -511,6 +511,30 @@ static bool same_rows(const pf_rows& a, const pf_rows& b) {
   return a.p == b.p && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
 }
 
+// A buffer of a call by its whole extent (p NULL: there is none).
+struct Extent {
+  const void* p;
+  size_t bytes;
+};
+
+static Extent extent_of(const pf_rows* r, int64_t n, int heads, const HeadsDims& d) {
+  return r && n > 0 ? Extent{r->p, rows_bytes(*r, n, heads, d)} : Extent{nullptr, 0};
+}
+
+// Whether any of the `nw` buffers at `w` meets one behind it or one of `r`.
+static bool any_meet(const Extent* w, int nw, const Extent* r, int nr) {
+  auto meet = [](const Extent& a, const Extent& b) {
+    return a.p && b.p && a.bytes && b.bytes && overlaps(a.p, a.bytes, b.p, b.bytes);
+  };
+  for (int i = 0; i < nw; ++i) {
+    for (int j = i + 1; j < nw; ++j)
+      if (meet(w[i], w[j])) return true;
+    for (int j = 0; j < nr; ++j)
+      if (meet(w[i], r[j])) return true;
+  }
+  return false;
+}
+
 static int check_heads(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n, HeadsDims* d,
                        HeadsWeights* hw) {
   const char* why;
@@ -598,6 +622,16 @@ int proxy_qk_norm_rope_backward(const pf_heads_config* cfg, const pf_heads_weigh
     if (!workspace || ws_bytes < need)
       return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need, workspace ? ws_bytes : 0);
     if (!aligned16(workspace)) return fail(PF_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const size_t gain = (size_t)d.d * sizeof(float), gain_in = (size_t)d.d * d.esize;
+    const Extent wr[3] = {{dgamma_q, gain}, {dgamma_k, gain}, {workspace, need}};
+    const Extent rd[10] = {extent_of(q, n, d.hq, d),      extent_of(k, n, d.hk, d),
+                           extent_of(dq_out, n, d.hq, d), extent_of(dk_out, n, d.hk, d),
+                           extent_of(dq, n, d.hq, d),     extent_of(dk, n, d.hk, d),
+                           {w->gamma_q, gain_in},         {w->gamma_k, gain_in},
+                           {w->freqs, (size_t)(d.rot / 2) * sizeof(double)},
+                           {positions, (size_t)d.n_axes * n * sizeof(int32_t)}};
+    if (any_meet(wr, 3, rd, 10))
+      return fail(PF_ERR_INVALID_ARG, "gain gradients and workspace must not overlap other buffers of the call");
   }
   return hip_status(launch_qk_backward(d, hw, n, rows_of(q), rows_of(k), positions, rows_of(dq_out), rows_of(dk_out),
                                        rows_of(dq), rows_of(dk), dgamma_q, dgamma_k, static_cast<float*>(workspace),
@@ -703,12 +737,21 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
   if (!out) return fail(PF_ERR_INVALID_ARG, "out is NULL");
   if (!aligned16(out)) return fail(PF_ERR_INVALID_ARG, "out must be 16-byte aligned");
   if (!aligned4(lse)) return fail(PF_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-  const size_t out_bytes = (size_t)n * d.hq * d.d * d.esize;
-  if (overlaps(out, out_bytes, q->p, rows_bytes(*q, n, d.hq, d)))
-    return fail(PF_ERR_INVALID_ARG, "out must not overlap q");
   if (pl.bytes && (!workspace || ws_bytes < pl.bytes))
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", pl.bytes, workspace ? ws_bytes : 0);
   if (!aligned16(workspace)) return fail(PF_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  const size_t pages = (size_t)c.n_pages * d.hk * c.page_size * d.d * d.esize;
+  const Extent wr[3] = {{out, (size_t)n * d.hq * d.d * d.esize},
+                        {lse, (size_t)n * d.hq * sizeof(float)},
+                        {workspace, pl.bytes}};
+  const Extent rd[6] = {extent_of(q, n, d.hq, d),
+                        {c.k, pages},
+                        {c.v, pages},
+                        {cache->page_table, (size_t)c.batch * cache->max_pages * sizeof(int32_t)},
+                        {cache->kv_len, (size_t)c.batch * sizeof(int32_t)},
+                        {cu_tokens, ((size_t)c.batch + 1) * sizeof(int32_t)}};
+  if (any_meet(wr, 3, rd, 6))
+    return fail(PF_ERR_INVALID_ARG, "out, lse and workspace must not overlap other buffers of the call");
   return hip_status(launch_paged_attention(d, c, pl, n, cu_tokens, rows_of(q), scale, window, sinks, out, lse,
                                            static_cast<char*>(workspace), reinterpret_cast<hipStream_t>(stream)),
                     "proxy_paged_attention launch");

@@ -151,6 +151,27 @@ def test_overlaps():
     refused(attend(out=P + 512))
 
 
+def test_outputs_and_workspaces_apart():
+    refused(attend(out=16 * P + 1024))                # on the pages it reads
+    refused(attend(out=32 * P))
+    refused(attend(lse=5 * P + 64))                   # on out
+    refused(attend(lse=P + 16))                       # on the queries
+    refused(attend(lse=32 * P + 16))                  # on the pages
+    need = B.load().proxy_paged_workspace_size(cfg(), 3, 3, 0, 1, 4000, 0, 0)
+    assert 0 < need < 8 * P
+    for ws in (P, 5 * P, 16 * P, 64 * P - 256):       # queries, out, pages, lse
+        refused(attend(max_kv=4000, ws=ws, lse=64 * P))
+    refused(attend(max_kv=4000, ca=cache(page_table=6 * P + 16)))
+    refused(attend(max_kv=4000, ca=cache(kv_len=6 * P + 16)))
+    for at in (P, 2 * P, 3 * P, 4 * P, 8 * P, 9 * P):  # any rows of the call
+        refused(backward(gq=at + 64))
+        refused(backward(gk=at + 64))
+        refused(backward(ws=at))
+    refused(backward(gq=5 * P, gk=5 * P + 128))
+    refused(backward(gq=7 * P))                       # on the workspace
+    refused(backward(gk=7 * P + 16))
+
+
 @pytest.mark.parametrize("bad", [
     dict(k_pages=None), dict(v_pages=None), dict(page_table=None), dict(kv_len=None), dict(k_pages=16 * P + 8),
     dict(page_table=P + 2), dict(kv_len=P + 1), dict(batch=0), dict(n_pages=0), dict(max_pages=0), dict(page_size=0),
