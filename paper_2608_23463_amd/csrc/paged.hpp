@@ -83,19 +83,19 @@ struct Sight {
   int head_tiles;   // tiles that hold the first rows
   int gap;          // added to later tile numbers
   int tiles;
-  __device__ __forceinline__ Sight(const PagedParams& p, const Sequence& sq, int x0, int cols, int tile_rows) {
+  __host__ __device__ __forceinline__ Sight(const PagedParams& p, const Sequence& sq, int x0, int cols, int tile_rows) {
     first = max(sq.row0 + p.fgroup.div(x0), 0);
     top = max(sq.row0 + p.fgroup.div(x0 + cols - 1), -1);
     last = min(top, sq.most - 1);
     const int lo = max(first - p.window + 1, 0), n = last + 1;
-    head_tiles = (min(p.sinks, lo) + tile_rows - 1) / tile_rows;
+    head_tiles = (min(min(p.sinks, lo), sq.most) + tile_rows - 1) / tile_rows;  // (lengths may pass the table)
     gap = max(lo / tile_rows - head_tiles, 0);
     const int all = (n + tile_rows - 1) / tile_rows;  // (the windows may lie past the table's end)
     tiles = min(head_tiles, all) + max(all - head_tiles - gap, 0);
   }
-  __device__ __forceinline__ int tile(int i) const { return i < head_tiles ? i : i + gap; }
+  __host__ __device__ __forceinline__ int tile(int i) const { return i < head_tiles ? i : i + gap; }
   // As many slices as leave each min_tiles, all of the same size but the last.
-  __device__ __forceinline__ int per_slice(const PagedParams& p) const {
+  __host__ __device__ __forceinline__ int per_slice(const PagedParams& p) const {
     const int n = max(min(p.fmin_tiles.div(tiles), p.slices), 1);
     return max((tiles + n - 1) / n, 1);
   }
