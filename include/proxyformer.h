@@ -463,6 +463,8 @@ int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, co
  * result with another attention's. A token that sees nothing (an empty slot):
  * out is zero and lse -inf. Tokens behind the last sequence: out and lse are
  * left as they were. The norm and the rotation of cfg are not applied here.
+ * Values of a magnitude below 2^80 give finite results, whatever the finite
+ * scores: weighted sums are fp32 and divided by their weights' sum at the end.
  * A row that a token does not see has no weight in its result; of the rows
  * that other tokens of the same call see it is taken times zero, so an
  * infinity or a NaN in one of those can reach it.

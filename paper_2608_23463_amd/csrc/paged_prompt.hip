@@ -138,10 +138,12 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
     for (int r = 0; r < 16; ++r) o[cb][r] = 0.0f;
   // Scores in exp2 units against a reference: a real maximum of the lane
   // pair's first tile with a visible row, kept while the running sums stay
-  // below 2^64, then raised.
+  // below 2^32, then raised: weights and sums of values of up to 2^80 are far
+  // from fp32's end, also where 512 slices are joined, and a reference that is
+  // near the maximum (the rows of a long cache add 2^10 to 2^20) stays.
   float mref = -INFINITY, lrun = 0.0f;
   bool have_ref = false;  // wave-uniform
-  constexpr float kSumLimit = 18446744073709551616.0f;  // 2^64
+  constexpr float kSumLimit = 4294967296.0f;  // 2^32
 
   int rows = -1, rows_next = -1;  // of 16 tiles, and of the 16 behind them
   if (ntiles > 0) {

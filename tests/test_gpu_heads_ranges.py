@@ -1,0 +1,59 @@
+"""The fine tokens' own attention on the GPU where its kernels change course:
+references of a softmax that have to be raised, values far from one, sums over
+many steps. Oracle and tolerances are those of test_gpu_heads.py."""
+import numpy as np
+import pytest
+
+from oracle import heads as O
+from helpers import dev, host
+from test_gpu_heads import E, U, Paged, check_attend, close, draw
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- softmax references
+
+def rising(rng, p, lens, new, hq, d, rise, step):
+    """Keys and queries of which every third token's even heads score `rise`
+    (units of log2) more at the last rows than at the first 64, in one step or
+    row by row, and the others about the same everywhere: u.u = d, q = 2 u, so
+    a row a u adds 2 a sqrt(d) log2(e)."""
+    u = np.sign(rng.standard_normal(d)).astype(np.float32)
+    for b, n in enumerate(lens):
+        for j in range(n):
+            share = 0.0 if j < 64 else 1.0 if step else (j - 64) / (n - 64)
+            pg = p.table[b, j // p.page]
+            k = rng.standard_normal((p.k.shape[1], d)) * 0.5 + share * rise / (2 * np.sqrt(d) * np.log2(np.e)) * u
+            p.k[pg, :, j % p.page] = np.float32(dev(k.astype(np.float32), "bf16").float().cpu().numpy())
+    t = sum(new)
+    q = rng.standard_normal((t, hq, d)) * 0.05
+    q[1::3, ::2] += 2 * u
+    return dev(q.astype(np.float32), "bf16").float().cpu().numpy()
+
+
+@pytest.mark.parametrize("step", [True, False], ids=["step", "slope"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 3)])
+@pytest.mark.parametrize("rise", [20, 60, 250])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_that_rise(gpu, d, rise, window, sinks, step):
+    """Later keys score far above a prompt's first tile, for some columns of a
+    wave: sums below, at and past every limit on them, up to exponentials that
+    are infinite against the first reference. Whole and cut into slices; values
+    of 1 and of 2^70, whose weighted sums stay finite only against a reference
+    near the maximum."""
+    import torch
+    rng = np.random.default_rng(21)
+    hq, lens, new = 4, [390, 200], [160, 200]
+    p = Paged(gpu, rng, hq, 2, d, "bf16", 16, lens, lens)
+    q = rising(rng, p, lens, new, hq, d, rise, step)
+    p.kd.copy_(dev(p.k, "bf16"))
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    for size in (1.0, 2.0 ** 70):
+        p.v *= np.float32(size)
+        p.vd.copy_(dev(p.v, "bf16"))
+        for longest in (64, 3000):  # one slice, several
+            lse = torch.full((sum(new), hq), float("nan"), device="cuda")
+            out = p.cache.attend(dev(q, "bf16"), longest, cu_tokens=torch.from_numpy(cu).cuda(), max_new=max(new),
+                                 window=window, sinks=sinks, lse=lse)
+            torch.cuda.synchronize()
+            check_attend(p, q, out, lse, cu, window, sinks, d ** -0.5, (rise, size, longest), max(new))
