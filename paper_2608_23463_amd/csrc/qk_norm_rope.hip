@@ -381,20 +381,27 @@ struct QkBwdParams {
 
 // dz = R(-t) dy; dgamma += dz * xn with xn = x rstd; g = dz gamma;
 // dx = rstd (g - xn mean(g xn)). A lane keeps the gains' gradients of its 16
-// elements over all its rows; the workgroups' sums are joined in a fixed order.
+// elements over kGainRows of its rows; then its wave's lanes are joined and
+// added to sums in 64 bits, so that the error does not grow with the tokens.
+// The workgroups' sums are joined in a fixed order.
+constexpr int kGainRows = 64;
+
 template <typename T, int D, bool PAIRS, int TPW>
 __global__ void __launch_bounds__(kThreads, 3) qk_backward_kernel(QkBwdParams p) {
   constexpr int LPR = D / 16, RPP = kWave / LPR;
   __shared__ float2 turns[kWaves][TPW][D / 2];
-  __shared__ float sums[kWaves][D];
+  __shared__ double sums[kWaves][2][D];
   __shared__ float gains[2][D];
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   const int row = lane / LPR;
   const Chunk<D, PAIRS> ch(lane % LPR, p.turn.rot);
   float acc[2][16] = {};
+  int rows = 0;  // of a lane since the last fold, at most
   for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
     const T* gamma = static_cast<const T*>(i < D ? p.gamma_q : p.gamma_k);
     gains[i / D][i % D] = p.norm && gamma ? to_f32(gamma[i % D]) : 1.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sums[w][i / D][i % D] = 0.0;
   }
   __syncthreads();
   const int64_t step = (int64_t)gridDim.x * kWaves * TPW;
@@ -456,25 +463,38 @@ __global__ void __launch_bounds__(kThreads, 3) qk_backward_kernel(QkBwdParams p)
     };
     run(p.q, p.dqo, p.dq, gains[0], p.hq, p.fq, acc[0]);
     run(p.k, p.dko, p.dk, gains[1], p.hk, p.fk, acc[1]);
+    rows += (TPW * p.hq + RPP - 1) / RPP;
+    if (p.part && (rows >= kGainRows || t0 + step >= p.turn.n)) {
+      rows = 0;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+#pragma unroll
+        for (int o = LPR; o < kWave; o <<= 1)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[w][i] += __shfl_xor(acc[w][i], o);
+        if (row == 0)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            double* to = &sums[wave][w][half ? ch.b : ch.a];
+            double v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = to[i] + acc[w][8 * half + i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[i] = v[i];
+          }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[w][i] = 0.0f;
+      }
+    }
   }
-  if (!p.norm || !p.part) return;
+  if (!p.part) return;
+  __syncthreads();
+  if (threadIdx.x < 2 * D) {
+    const int w = threadIdx.x / D, c = threadIdx.x % D;
+    double v = 0.0;
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = acc[w][i];
-#pragma unroll
-      for (int o = LPR; o < kWave; o <<= 1) v += __shfl_xor(v, o);
-      if (row == 0) sums[wave][i < 8 ? ch.a + i : ch.b + i - 8] = v;
-    }
-    __syncthreads();
-    if (threadIdx.x < D) {
-      float v = 0.0f;
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) v += sums[k][threadIdx.x];
-      p.part[((int64_t)w * gridDim.x + blockIdx.x) * D + threadIdx.x] = v;
-    }
-    __syncthreads();
+    for (int k = 0; k < kWaves; ++k) v += sums[k][w][c];
+    p.part[((int64_t)w * gridDim.x + blockIdx.x) * D + c] = (float)v;
   }
 }
 

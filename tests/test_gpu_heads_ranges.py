@@ -57,3 +57,35 @@ def test_scores_that_rise(gpu, d, rise, window, sinks, step):
                                  window=window, sinks=sinks, lse=lse)
             torch.cuda.synchronize()
             check_attend(p, q, out, lse, cu, window, sinks, d ** -0.5, (rise, size, longest), max(new))
+
+
+# ---------------------------------------------------------------- gains' gradients
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_gain_gradients_of_millions_of_tokens(gpu, dtype):
+    """Four million equal tokens of 16 heads (the same row read with strides of
+    0): every partial sum of a chain rounds the same way, so an error that grows
+    with its length shows. Per element: a term 40 E; chains of 64 rows and those
+    of one step, the sums of a workgroup in 64 bits, one rounding, then 768
+    workgroups' sums in chains of 6, a tree of 3 and 16 streams: 40 + 66 + 1 + 25
+    and some, 136 E of the terms' magnitudes."""
+    import torch
+    B = gpu
+    rng = np.random.default_rng(22)
+    t, hq, d = 1 << 22, 16, 64
+    if dtype == "fp32":
+        t //= 2
+        hq *= 2
+    cfg = B.heads_config(hq, 1, d, dtype=dtype, rot_dim=0)
+    rows = {x: draw(rng, (1, 1, d), dtype) for x in ("q", "k", "dq", "dk")}
+    gamma = draw(rng, d, dtype)
+    wide = {x: dev(a, dtype).expand(t, 1 if "k" in x else hq, d) for x, a in rows.items()}
+    got = B.qk_norm_rope_backward(cfg, {"gamma_q": dev(gamma, dtype), "gamma_k": dev(gamma, dtype)}, wide["q"], wide["k"],
+                                  None, wide["dq"], wide["dk"])
+    torch.cuda.synchronize()
+    for i, (x, n) in enumerate((("q", t * hq), ("k", t))):
+        dx, dg, mag, dg_mag = O.norm_rope_backward(rows[x], gamma, 1e-6, True, np.zeros((1, 0)), 0, False, rows["d" + x])
+        first = got[i][:1, :1]
+        close(host(first), dx, U[dtype] * np.abs(dx) + 64 * E * mag, (x, "dx"))
+        assert torch.equal(got[i], first.expand_as(got[i]))
+        close(host(got[2 + i]), n * dg, 136 * E * n * dg_mag, (x, "gain"))
