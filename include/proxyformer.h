@@ -355,7 +355,8 @@ int proxy_decode_prefill(const pf_decode_config* cfg, const pf_decode_weights* w
  *            axis_pairs[1] by the second, ...; they add up to rot_dim / 2.
  * Pair p = (a, b) turns by t = coordinate * freqs[p]:
  *   y_a = z_a cos t - z_b sin t, y_b = z_a sin t + z_b cos t.
- * The angle is formed in 64 bits, so positions up to 2^31 keep it to 1e-6.
+ * The angle is formed in 64 bits and keeps to 2^-51 of itself: 1e-6 at 2^31
+ * radians.
  * Sums and statistics are fp32; a row is rounded once, when it is stored. */
 #define PF_MAX_AXES 3
 enum pf_head_norm { PF_NORM_NONE = 0, PF_NORM_RMS = 1 };

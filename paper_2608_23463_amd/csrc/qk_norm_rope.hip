@@ -121,14 +121,16 @@ struct QkParams {
 
 // Cosine and sine of position * frequency. Far positions need more than 32
 // bits: a position of 2^20 in fp32 leaves an angle off by up to 2^-4. The
-// angle is formed in revolutions in 64 bits and its whole revolutions dropped
-// there, so what fp32 sees is below half a revolution and off by at most 2^-26.
+// angle is formed in revolutions in 64 bits (three roundings: 2^-51 of it) and
+// its whole revolutions dropped there. What rounding the rest to fp32 leaves, up
+// to 2^-26 of a revolution, is turned by to first order.
 __device__ __forceinline__ float2 turn_of(double freq, int pos) {
   const double rev = (double)pos * freq * 0.15915494309189533577;
-  const float f = (float)(rev - rint(rev));
-  float2 cs;
-  sincospif(2.0f * f, &cs.y, &cs.x);
-  return cs;
+  const double part = rev - rint(rev);
+  const float f = (float)part, rest = (float)((part - f) * 6.28318530717958647693);
+  float s, c;
+  sincospif(2.0f * f, &s, &c);
+  return make_float2(c - rest * s, s + rest * c);
 }
 
 __device__ __forceinline__ int axis_of(const TurnParams& t, int pair) {

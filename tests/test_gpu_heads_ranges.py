@@ -89,3 +89,31 @@ def test_gain_gradients_of_millions_of_tokens(gpu, dtype):
         close(host(first), dx, U[dtype] * np.abs(dx) + 64 * E * mag, (x, "dx"))
         assert torch.equal(got[i], first.expand_as(got[i]))
         close(host(got[2 + i]), n * dg, 136 * E * n * dg_mag, (x, "gain"))
+
+
+# ---------------------------------------------------------------- angles
+
+@pytest.mark.parametrize("pos", [1, 12345, -(1 << 20)])
+def test_turns_near_the_axes(gpu, pos):
+    """Angles next to whole quarter turns, whose sine or cosine is close to 0:
+    the small one keeps its own digits. Rows (1, 0) of every pair give (cos,
+    sin). Per element: 16 E of itself (cosine and sine 4 E, doubled where what
+    fp32 leaves of the angle cancels half of it, and that term's roundings) and
+    the angle's three roundings in 64 bits, 4 x 2^-53 of it."""
+    import torch
+    B = gpu
+    d = 64
+    cfg = B.heads_config(1, 1, d, dtype="fp32", norm=False)
+    rng = np.random.default_rng(23)
+    quarter = np.arange(d // 2) % 8 + abs(pos) - 1  # close to whole quarters, of every sign and distance
+    ang = quarter * (np.pi / 2) + rng.standard_normal(d // 2) * 10.0 ** -(np.arange(d // 2) % 7 + 2)
+    freqs = ang / pos
+    x = torch.zeros(1, 1, d, device="cuda")
+    x[..., :d // 2] = 1
+    at = torch.full((1, 1), pos, dtype=torch.int32, device="cuda")
+    got = B.qk_norm_rope_forward(cfg, {"freqs": torch.from_numpy(freqs).cuda()}, x, x, at)
+    torch.cuda.synchronize()
+    ang = pos * freqs
+    ref = np.concatenate([np.cos(ang), np.sin(ang)])
+    for y in got:
+        close(host(y)[0, 0], ref, 16 * E * np.abs(ref) + 4 * 2.0 ** -53 * np.abs(np.concatenate([ang, ang])), pos)
