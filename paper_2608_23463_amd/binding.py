@@ -747,7 +747,9 @@ class PagedCache:
     k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim]; page_table
     int32 [batch, max_pages] and kv_len int32 [batch] on the device, the
     caller's own: it hands out pages and sets kv_len (the new tokens counted)
-    before a step's append, and the step's attention reads the same lengths."""
+    before a step's append, and the step's attention reads the same lengths.
+    cfg and weights are taken as they are when the cache is made: later changes
+    of the config or of the dict's entries do not reach it."""
 
     def __init__(self, cfg: PfHeadsConfig, weights: Dict[str, object], k_pages, v_pages, page_table, kv_len):
         import torch
@@ -756,9 +758,10 @@ class PagedCache:
             raise ValueError(f"tensors must be on a GPU, got {dev}")
         shape = (k_pages.shape[0], cfg.n_kv_heads, None, cfg.head_dim)
         batch = kv_len.shape[0]
-        self.cfg = cfg
+        self.cfg = PfHeadsConfig.from_buffer_copy(cfg)
         self.device = dev
-        self.tensors = (k_pages, v_pages, page_table, kv_len, weights)  # kept alive
+        self.tensors = (k_pages, v_pages, page_table, kv_len)  # kept alive, like the weights as they are now
+        self.weights = dict(weights)
         self.batch = batch
         self.wstruct = _heads_weights(cfg, weights, dev)
         self.state = PfPagedCache(_want("k_pages", k_pages, dt, dev, shape),

@@ -117,3 +117,24 @@ def test_turns_near_the_axes(gpu, pos):
     ref = np.concatenate([np.cos(ang), np.sin(ang)])
     for y in got:
         close(host(y)[0, 0], ref, 16 * E * np.abs(ref) + 4 * 2.0 ** -53 * np.abs(np.concatenate([ang, ang])), pos)
+
+
+# ---------------------------------------------------------------- what a cache holds
+
+def test_cache_keeps_its_weights(gpu):
+    """A cache goes on with the config, gains and frequencies that it was made
+    with when the caller changes the config, or empties the dict or gives it
+    others."""
+    import gc
+    import weakref
+    import torch
+    p = Paged(gpu, np.random.default_rng(24), 4, 2, 64, "bf16", 16, [20], [20], norm=True, rot=64)
+    w = {name: t.clone() for name, t in p.weights.items()}
+    cache = gpu.PagedCache(p.cfg, w, p.kd, p.vd, p.td, p.ld)
+    held = {name: weakref.ref(t) for name, t in w.items()}
+    w["gamma_q"] = torch.zeros(64, dtype=torch.bfloat16, device="cuda")
+    del w["gamma_k"], w["freqs"]
+    gc.collect()
+    p.cfg.head_dim = 128
+    assert cache.cfg.head_dim == 64
+    assert all(r() is not None for r in held.values()), [n for n, r in held.items() if r() is None]
