@@ -383,7 +383,8 @@ typedef struct {
  * negative; rows 16-byte aligned, so multiples of 8 in bf16 and 4 in fp32): a
  * slice of a fused projection, or heads-first storage. Rows that a call
  * writes must not share elements with each other. They may be the very rows
- * they are computed from (same p and strides); other overlaps are refused. */
+ * they are computed from (same p and strides); other overlaps are refused, also
+ * with what else the call reads (gains, freqs, positions, a cache's tables). */
 typedef struct {
   void* p;
   int64_t token_stride, head_stride;
@@ -448,7 +449,8 @@ typedef struct {
  *  token's row.
  * A token whose row has no page (an empty slot, a row before 0 or past the
  * table, an entry outside the cache) is left alone: neither cached nor its
- * query written. k and v must not overlap the pages. */
+ * query written. k and v must not overlap the pages, nor the pages and q_out
+ * anything else that the call reads. */
 int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_cache* cache,
                        int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
                        const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream);

@@ -535,6 +535,17 @@ static bool any_meet(const Extent* w, int nw, const Extent* r, int nr) {
   return false;
 }
 
+// What a call with a norm and a rotation reads beside its rows.
+struct SmallInputs {
+  Extent e[4];
+  SmallInputs(const HeadsDims& d, const HeadsWeights& w, const int32_t* positions, int64_t n)
+      : e{{d.norm ? w.gamma_q : nullptr, (size_t)d.d * d.esize},
+          {d.norm ? w.gamma_k : nullptr, (size_t)d.d * d.esize},
+          {d.rot ? w.freqs : nullptr, (size_t)(d.rot / 2) * sizeof(double)},
+          {d.rot ? positions : nullptr, (size_t)d.n_axes * n * sizeof(int32_t)}} {}
+  bool meets(const Extent& w) const { return any_meet(&w, 1, e, 4); }
+};
+
 static int check_heads(const pf_heads_config* cfg, const pf_heads_weights* w, int64_t n, HeadsDims* d,
                        HeadsWeights* hw) {
   const char* why;
@@ -573,6 +584,9 @@ int proxy_qk_norm_rope_forward(const pf_heads_config* cfg, const pf_heads_weight
       rows_meet(*k, d.hk, *q_out, d.hq, n, d) || rows_meet(*q, d.hq, *k_out, d.hk, n, d) ||
       rows_meet(*q_out, d.hq, *k_out, d.hk, n, d))
     return fail(PF_ERR_INVALID_ARG, "q_out and k_out must not overlap other rows of the call");
+  const SmallInputs small(d, hw, positions, n);
+  if (small.meets(extent_of(q_out, n, d.hq, d)) || small.meets(extent_of(k_out, n, d.hk, d)))
+    return fail(PF_ERR_INVALID_ARG, "q_out and k_out must not overlap gains, freqs or positions");
   return hip_status(launch_qk_forward(d, hw, n, rows_of(q), rows_of(k), positions, rows_of(q_out), rows_of(k_out),
                                       reinterpret_cast<hipStream_t>(stream)),
                     "proxy_qk_norm_rope_forward launch");
@@ -616,6 +630,9 @@ int proxy_qk_norm_rope_backward(const pf_heads_config* cfg, const pf_heads_weigh
         return fail(PF_ERR_INVALID_ARG, "dq and dk must not overlap other rows of the call");
     }
     if (rows_meet(*dq, d.hq, *dk, d.hk, n, d)) return fail(PF_ERR_INVALID_ARG, "dq and dk must not overlap");
+    const SmallInputs small(d, hw, positions, n);
+    if (small.meets(extent_of(dq, n, d.hq, d)) || small.meets(extent_of(dk, n, d.hk, d)))
+      return fail(PF_ERR_INVALID_ARG, "dq and dk must not overlap gains, freqs or positions");
   }
   const size_t need = qk_backward_ws(d, n);
   if (need && (dgamma_q || dgamma_k)) {
@@ -694,6 +711,13 @@ int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, co
     if (on_pages(q, d.hq) || on_pages(q_out, d.hq)) return fail(PF_ERR_INVALID_ARG, "q and q_out must not overlap the pages");
   }
   if (on_pages(k, d.hk) || on_pages(v, d.hk)) return fail(PF_ERR_INVALID_ARG, "k and v must not overlap the pages");
+  const SmallInputs small(d, hw, positions, n);
+  const Extent tables[3] = {{c.table, (size_t)c.batch * c.max_pages * sizeof(int32_t)},
+                            {c.kv_len, (size_t)c.batch * sizeof(int32_t)},
+                            {cu_tokens, ((size_t)c.batch + 1) * sizeof(int32_t)}};
+  for (const Extent& w : {with_q ? extent_of(q_out, n, d.hq, d) : Extent{nullptr, 0}, Extent{c.k, pages}, Extent{c.v, pages}})
+    if (small.meets(w) || any_meet(&w, 1, tables, 3))
+      return fail(PF_ERR_INVALID_ARG, "q_out and the pages must not overlap gains, freqs, positions, table or lengths");
   return hip_status(launch_paged_append(d, hw, c, n, cu_tokens, with_q ? rows_of(q) : Rows{}, rows_of(k), rows_of(v),
                                         positions, with_q ? rows_of(q_out) : Rows{},
                                         reinterpret_cast<hipStream_t>(stream)),
