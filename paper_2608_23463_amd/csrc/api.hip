@@ -487,9 +487,12 @@ static size_t rows_bytes(const pf_rows& r, int64_t n, int heads, const HeadsDims
   return (size_t)((n - 1) * r.token_stride + (heads - 1) * r.head_stride + d.d) * d.esize;
 }
 
-// Whether two sets of rows may share elements. Bands of one buffer with the
-// same stride (the slices of a fused projection) are told apart within a
-// period of that stride; everything else by its whole extent.
+// Whether two sets of rows may share elements. Bands of one buffer that share a
+// stride (the slices of a fused projection) are told apart within a period of
+// it. Other sets with the same strides (heads whose q, k and v lie side by side)
+// are compared row by row: token t', head h' of b begins delta + dt ts + dh hs
+// past token t, head h of a, with dt = t' - t and dh = h' - h, and rows meet
+// that begin less than head_dim apart. What is left goes by its whole extent.
 static bool rows_meet(const pf_rows& a, int ha, const pf_rows& b, int hb, int64_t n, const HeadsDims& d) {
   if (!overlaps(a.p, rows_bytes(a, n, ha, d), b.p, rows_bytes(b, n, hb, d))) return false;
   const int64_t delta = (reinterpret_cast<intptr_t>(b.p) - reinterpret_cast<intptr_t>(a.p)) / d.esize;
@@ -504,7 +507,17 @@ static bool rows_meet(const pf_rows& a, int ha, const pf_rows& b, int hb, int64_
   if (a.head_stride == b.head_stride &&
       apart(a.head_stride, (n - 1) * a.token_stride + d.d, (n - 1) * b.token_stride + d.d))
     return false;
-  return true;
+  const bool same_hs = a.head_stride == b.head_stride || ha == 1 || hb == 1;
+  if (!same_hs || (n > 1 && (a.token_stride != b.token_stride || a.token_stride < d.d))) return true;
+  const int64_t ts = n == 1 ? 0 : a.token_stride, hs = ha > 1 ? a.head_stride : b.head_stride;
+  for (int dh = 1 - ha; dh < hb; ++dh) {
+    const int64_t x = delta + dh * hs;
+    // the dt that leaves 0 <= r < ts, and the one below it
+    const int64_t dt = ts ? (x >= 0 ? -(x / ts) : (-x + ts - 1) / ts) : 0, r = x + dt * ts;
+    if (r > -d.d && r < d.d && dt > -n && dt < n) return true;
+    if (ts && r - ts > -d.d && dt - 1 > -n && dt - 1 < n) return true;
+  }
+  return false;
 }
 
 static bool same_rows(const pf_rows& a, const pf_rows& b) {

@@ -138,3 +138,55 @@ def test_cache_keeps_its_weights(gpu):
     p.cfg.head_dim = 128
     assert cache.cfg.head_dim == 64
     assert all(r() is not None for r in held.values()), [n for n, r in held.items() if r() is None]
+
+
+# ---------------------------------------------------------------- layouts
+
+@pytest.mark.parametrize("t", [1, 33])
+@pytest.mark.parametrize("order", ["head", "part"])
+def test_projections_with_interleaved_heads(gpu, order, t):
+    """q, k and v of one buffer whose heads hold their three rows side by side
+    ([T, H, 3, D]), or whose rows hold their heads heads-first ([3, H, T, D]):
+    normed and turned in place, forward, backward and append, as apart."""
+    import torch
+    B = gpu
+    rng = np.random.default_rng(25)
+    h, d, page = 6, 64, 16
+    cfg = B.heads_config(h, h, d)
+    w = {"gamma_q": dev(draw(rng, d, "bf16"), "bf16"), "gamma_k": dev(draw(rng, d, "bf16"), "bf16"),
+         "freqs": B.rope_freqs(cfg)}
+    pos = torch.arange(t, dtype=torch.int32, device="cuda")
+
+    def buffer():
+        if order == "head":
+            b = dev(draw(rng, (t, h, 3, d), "bf16"), "bf16")
+            return b, b.unbind(2)
+        b = dev(draw(rng, (3, h, t, d), "bf16"), "bf16")
+        return b, [x.transpose(0, 1) for x in b.unbind(0)]
+
+    whole, (q, k, v) = buffer()
+    grads, (dq, dk, _) = buffer()
+    apart = [x.contiguous().clone() for x in (q, k, v, dq, dk)]
+    want = B.qk_norm_rope_forward(cfg, w, apart[0], apart[1], pos)
+    want_d = B.qk_norm_rope_backward(cfg, w, apart[0], apart[1], pos, apart[3], apart[4])
+    got_d = B.qk_norm_rope_backward(cfg, w, q, k, pos, dq, dk, dq=dq, dk=dk)
+    for x, y in zip(got_d, want_d):
+        assert torch.equal(x, y)
+
+    def cache():
+        pages = [torch.zeros(4, h, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        return pages, B.PagedCache(cfg, w, *pages, torch.arange(4, dtype=torch.int32, device="cuda")[None],
+                                   torch.tensor([t], dtype=torch.int32, device="cuda"))
+
+    cu = torch.tensor([0, t], dtype=torch.int32, device="cuda")
+    pages, c = cache()
+    want_q = c.append(apart[1], apart[2], q=apart[0], cu_tokens=cu)
+    pages2, c2 = cache()
+    keep = whole.clone()
+    got_q = c2.append(k, v, q=q, cu_tokens=cu, q_out=q)
+    torch.cuda.synchronize()
+    assert torch.equal(got_q, want_q) and all(torch.equal(x, y) for x, y in zip(pages, pages2))
+    whole.copy_(keep)
+    B.qk_norm_rope_forward(cfg, w, q, k, pos, q, k)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, apart[2])

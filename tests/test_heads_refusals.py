@@ -45,3 +45,15 @@ def test_append_on_its_tables():
     refused(append(cu=4 * P + 64))
     refused(append(cu=16 * P + 64))
     refused(append(cu=32 * P + 64))
+
+
+def test_rows_side_by_side_that_meet():
+    """Heads whose rows lie three side by side: a step of less than a row meets
+    its neighbour, as does one that comes round to another head or token."""
+    c = cfg(n_heads=8, n_kv_heads=8)
+    side = lambda at, ts=8 * 192: rows(FAR + 2 * at, ts, 192)  # noqa: E731
+    for at in (0, 32, -32, 56, 192 + 8, 2 * 192, 7 * 192, 8 * 192, 8 * 192 + 32, -3 * 8 * 192 + 8):
+        refused(forward(c, q=side(0), qo=side(0), k=rows(2 * P), ko=side(at)))
+        refused(forward(c, q=side(0), qo=rows(3 * P, 8 * 64), k=rows(2 * P), ko=side(at)))
+    # tokens closer than a row (read only) count as meeting
+    refused(forward(c, q=rows(FAR, 8, 192), qo=rows(3 * P), k=rows(2 * P), ko=rows(FAR + 2 * 64, 8 * 192, 192)))
