@@ -763,7 +763,7 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
   if (!aligned4(cu_tokens)) return fail(PF_ERR_INVALID_ARG, "cu_tokens must be 4-byte aligned");
   if (max_new < 1 || max_kv_len < 1) return fail(PF_ERR_INVALID_ARG, "max_new and max_kv_len must be >= 1");
   if (window < 0 || sinks < 0) return fail(PF_ERR_INVALID_ARG, "window and sinks must be >= 0");
-  if (!std::isfinite(scale)) return fail(PF_ERR_INVALID_ARG, "scale must be finite");
+  if (!(std::fabs(scale) < 2.3e38f)) return fail(PF_ERR_INVALID_ARG, "scale must be finite and below 2.3e38");
   if (n_tokens == 0) return PF_OK;
   if (n_tokens > INT32_MAX / d.hq) return fail(PF_ERR_UNSUPPORTED, "n_tokens * n_heads above 2^28");
   const int64_t n = n_tokens;

@@ -57,3 +57,10 @@ def test_rows_side_by_side_that_meet():
         refused(forward(c, q=side(0), qo=rows(3 * P, 8 * 64), k=rows(2 * P), ko=side(at)))
     # tokens closer than a row (read only) count as meeting
     refused(forward(c, q=rows(FAR, 8, 192), qo=rows(3 * P), k=rows(2 * P), ko=rows(FAR + 2 * 64, 8 * 192, 192)))
+
+
+def test_scales_past_the_largest():
+    """The kernels take the scale times log2(e), which is infinite from 2.4e38 on."""
+    from test_heads_abi import attend
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        refused(attend(scale=scale))
