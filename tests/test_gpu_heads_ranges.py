@@ -6,7 +6,7 @@ import pytest
 
 from oracle import heads as O
 from helpers import dev, host
-from test_gpu_heads import E, U, Paged, check_attend, close, draw
+from test_gpu_heads import E, U, Paged, check_attend, close, draw, laid_out, qk_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -190,3 +190,101 @@ def test_projections_with_interleaved_heads(gpu, order, t):
     B.qk_norm_rope_forward(cfg, w, q, k, pos, q, k)
     torch.cuda.synchronize()
     assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, apart[2])
+
+
+# ---------------------------------------------------------------- many tokens
+
+def one_token_per_wave(t, d, *heads):
+    """Whether a call takes a token per wave: 2,048 tokens or more whose rows fill
+    the wave's passes of 1024 / head_dim rows to two thirds."""
+    passes = sum(-(-h * d // 1024) for h in heads)
+    return t >= 2048 and 2 * passes * (1024 // d) <= 3 * sum(heads)
+
+
+MANY = {
+    # as in test_gpu_heads.CASES; each fills its passes
+    "T2048_h16_16x64": (2048, 16, 16, 64, "bf16", True, 64, False, (32,), "band"),
+    "T2055_h16_4x128_pairs": (2055, 16, 4, 128, "bf16", True, 128, True, (20, 30, 14), "plain"),
+    "T2051_h16x64_fp32_pairs": (2051, 16, 16, 64, "fp32", True, 48, True, (24,), "heads"),
+    "T2049_h16_8x128_fp32": (2049, 16, 8, 128, "fp32", True, 128, False, (64,), "band"),
+    "T2050_h32_16x64_no_norm": (2050, 32, 16, 64, "bf16", False, 32, True, (16,), "plain"),
+}
+
+
+@pytest.mark.parametrize("name", MANY)
+def test_forward_of_many_tokens(gpu, name):
+    import torch
+    t, hq, hk, d, dtype, norm, rot, pairs, axes, layout = MANY[name]
+    assert one_token_per_wave(t, d, hq, hk)
+    a = qk_inputs(gpu, MANY[name], 26)
+    got = gpu.qk_norm_rope_forward(a["cfg"], a["w"], laid_out(a["q"], dtype, layout), laid_out(a["k"], dtype, layout), a["pos"])
+    torch.cuda.synchronize()
+    for y, x, g in ((got[0], a["q"], a["g"][0]), (got[1], a["k"], a["g"][1])):
+        ref, mag = O.norm_rope(x, g, 1e-5, norm, a["ang"], rot, pairs)
+        close(host(y), ref, U[dtype] * np.abs(ref) + 32 * E * mag, name)
+
+
+STEPS = {
+    # 768 workgroups of eight tokens: 6,144 in a step of the backward
+    "T6144_h4_2x64": (6144, 4, 2, 64, "bf16", True, 64, False, (32,), "plain"),
+    "T6151_h5_1x128_fp32_pairs": (6151, 5, 1, 128, "fp32", True, 128, True, (64,), "band"),
+    "T13001_h4_4x64_axes": (13001, 4, 4, 64, "bf16", True, 32, False, (5, 11), "heads"),
+    "T12289_h3x64_fp32_no_norm": (12289, 3, 3, 64, "fp32", False, 64, False, (32,), "plain"),
+    "T6145_h20x128": (6145, 20, 20, 128, "bf16", True, 128, False, (64,), "plain"),
+}
+
+
+@pytest.mark.parametrize("name", STEPS)
+def test_backward_of_several_steps(gpu, name):
+    import torch
+    t, hq, hk, d, dtype, norm, rot, pairs, axes, layout = STEPS[name]
+    a = qk_inputs(gpu, STEPS[name], 27)
+    x = {n: laid_out(a[n], dtype, layout) for n in ("q", "k", "dq", "dk")}
+    got = gpu.qk_norm_rope_backward(a["cfg"], a["w"], x["q"], x["k"], a["pos"], x["dq"], x["dk"])
+    again = gpu.qk_norm_rope_backward(a["cfg"], a["w"], x["q"], x["k"], a["pos"], x["dq"], x["dk"], dq=x["dq"], dk=x["dk"])
+    torch.cuda.synchronize()
+    for y, z in zip(got, again):
+        assert (y is None and z is None) or torch.equal(y, z)
+    for i, n in enumerate(("q", "k")):
+        dx, dg, mag, dg_mag = O.norm_rope_backward(a[n], a["g"][i], 1e-5, norm, a["ang"], rot, pairs, a["d" + n])
+        close(host(got[i]), dx, U[dtype] * np.abs(dx) + 64 * E * mag, (name, n))
+        if norm:
+            close(host(got[2 + i]), dg, 128 * E * dg_mag, (name, "gain", n))
+
+
+@pytest.mark.parametrize("case", [(32, 8, 128, "bf16", 16, False), (16, 16, 64, "fp32", 48, True), (16, 4, 128, "bf16", 64, True)],
+                         ids=str)
+def test_append_of_many_tokens(gpu, case):
+    """Prompts of more than 2,048 tokens together, with padding behind them, a
+    token per wave: rows of the pages and queries against the oracle, the rest
+    as it was."""
+    import torch
+    hq, hk, d, dtype, page, pairs = case
+    rng = np.random.default_rng(28)
+    lens, new, pad = [1500, 40, 900, 16], [1400, 0, 700, 16], 9
+    p = Paged(gpu, rng, hq, hk, d, dtype, page, lens, [0] * 4, norm=True, rot=d, pairs=pairs)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    t = int(cu[-1]) + pad
+    assert one_token_per_wave(t, d, hq, hk, hk)
+    q, k, v = draw(rng, (t, hq, d), dtype), draw(rng, (t, hk, d), dtype), draw(rng, (t, hk, d), dtype)
+    qo = torch.full((t, hq, d), 7.0, dtype=p.kd.dtype, device="cuda")
+    cud = torch.from_numpy(cu).cuda()
+    p.cache.append(laid_out(k, dtype, "band"), laid_out(v, dtype, "heads"), q=laid_out(q, dtype, "band"), q_out=qo, cu_tokens=cud)
+    kd, vd = p.kd.clone(), p.vd.clone()
+    p.kd.fill_(float("nan")), p.vd.fill_(float("nan"))
+    p.cache.append(dev(k, dtype), dev(v, dtype), cu_tokens=cud)  # without queries: 4 + 4 heads take four tokens
+    torch.cuda.synchronize()
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(p.kd.view(bits), kd.view(bits)) and torch.equal(p.vd.view(bits), vd.view(bits))
+    rows = O.token_rows(lens, cu)
+    n = len(rows)
+    ang = O.angles([[r for _, r in rows]], p.weights["freqs"].cpu().numpy(), [d // 2])
+    at = np.array([O.place(p.table[s], r, page, p.n_pages) for s, r in rows])
+    got_q, got_k, got_v = host(qo), host(kd), host(vd)
+    for x, g, y in ((q, p.gammas[0], got_q[:n]), (k, p.gammas[1], got_k[at[:, 0], :, at[:, 1]])):
+        ref, mag = O.norm_rope(x[:n], g, 1e-6, True, ang, d, pairs)
+        close(y, ref, U[dtype] * np.abs(ref) + 32 * E * mag, case)
+    assert (got_q[n:] == 7).all() and np.array_equal(got_v[at[:, 0], :, at[:, 1]], v[:n])
+    untouched = np.ones((p.n_pages, page), bool)
+    untouched[at[:, 0], at[:, 1]] = False
+    assert np.isnan(got_k.transpose(0, 2, 1, 3)[untouched]).all() and np.isnan(got_v.transpose(0, 2, 1, 3)[untouched]).all()
