@@ -419,9 +419,10 @@ int proxy_qk_norm_rope_backward(const pf_heads_config* cfg, const pf_heads_weigh
  *  multiple of 16, n_pages * n_kv_heads * page_size below 2^31
  *  page_table int32 [batch, max_pages]: page i of sequence b holds its rows
  *  i * page_size ..; max_pages * page_size at most 2^31 - 65536. Entries past
- *  a sequence's length are not read; an entry outside 0..n_pages-1 stands for
- *  no page: nothing is written there, and its rows are not seen. Sequences may
- *  share pages (of a common beginning) that no append writes.
+ *  a sequence's length may be read but have no effect; an entry outside
+ *  0..n_pages-1 stands for no page: nothing is written there, and its rows are
+ *  not seen. Sequences may share pages (of a common beginning) that no append
+ *  writes.
  *  kv_len int32 [batch]: rows of every sequence, those of the tokens being
  *  appended among them (one array serves a step's append and its attention in
  *  every layer). 0 or less: an empty slot.
@@ -473,15 +474,21 @@ int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, co
  * infinity or a NaN in one of those can reach it.
  *  max_new, max_kv_len (at least 1): most new tokens and rows of a sequence,
  *  which the launch is laid out for; larger ones are right but slower. The
- *  workspace goes by them.
+ *  workspace goes by them. In bf16 max_new also chooses how exact the weights
+ *  are in their product with the values: without cu_tokens or up to 31 they
+ *  keep 2^-16 of themselves, and the error is that of rounding the result; from
+ *  32 on they are rounded to bf16, 2^-8 (their sum before that), and the error
+ *  grows to 1.4 times that. Laid out for 31, prompts keep the exact weights
+ *  and take longer.
  *  workspace: proxy_paged_workspace_size bytes (`ragged`: whether cu_tokens is
  *  given), aligned to 256; 0 when no sequence is cut, and for invalid sizes.
  *  Calls that may run at the same time, graphs' replays among them, need
  *  workspaces of their own.
  *  out, lse and workspace overlap neither each other nor what the call reads.
- * n_tokens * n_heads below 2^28, batch * n_kv_heads below 2^24; n_tokens = 0
- * does nothing. The result does
- * not depend on where pages lie and is the same in every run. */
+ * n_tokens * n_heads / 16 + batch * n_kv_heads stays below 2^24 (without
+ * cu_tokens batch * n_kv_heads times the 16s that a group of heads begins);
+ * n_tokens = 0 does nothing. The result does not depend on where pages lie and is
+ * the same in every run. */
 size_t proxy_paged_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
                                   int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks);
 int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cache, int64_t n_tokens,

@@ -802,7 +802,9 @@ class PagedCache:
         over the rows up to their own: all of them, or (window > 0) the last
         `window` and the first `sinks`. max_kv_len, max_new: most rows and new
         tokens of a sequence, to lay the launch out for (max_new: 1 without
-        cu_tokens, T with it unless given). scale: 1 / sqrt(head_dim) unless
+        cu_tokens, T with it unless given; bf16 prompts laid out for 32 or more
+        round their weights to bf16, for 31 or fewer keep them in two terms,
+        more exact and slower). scale: 1 / sqrt(head_dim) unless
         given. lse: an fp32 [T, n_heads] tensor for the log-sums. workspace: a
         byte tensor that no call running at the same time uses (allocated
         unless given). Returns out; rows of tokens behind the last sequence are

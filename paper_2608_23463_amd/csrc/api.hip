@@ -769,7 +769,7 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
   const int64_t n = n_tokens;
   const PagedPlan pl = paged_plan(d, c.batch, n, cu_tokens != nullptr, max_new, max_kv_len, window, sinks);
   if (pl.groups > kMaxGroups / pl.slices)
-    return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes: n_tokens * n_heads must stay below 2^28");
+    return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes: n_tokens * n_heads / 16 + batch * n_kv_heads must stay below 2^24");
   if ((st = check_rows("q", q, n, d.hq, d, false)) != PF_OK) return st;
   if (!out) return fail(PF_ERR_INVALID_ARG, "out is NULL");
   if (!aligned16(out)) return fail(PF_ERR_INVALID_ARG, "out must be 16-byte aligned");

@@ -1,6 +1,6 @@
 // Attention of ordinary tokens beside the proxies: queries and keys normed
-// and turned by their positions, the paged cache they go to, and one token's
-// attention over it.
+// and turned by their positions, the paged cache they go to, and the attention
+// of new tokens, one of every sequence or a prompt, over it.
 #pragma once
 
 #include <stddef.h>

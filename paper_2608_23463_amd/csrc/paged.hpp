@@ -1,5 +1,5 @@
 // What the kernels of attention over a paged cache share: the call's
-// parameters, which rows a block of queries sees, and the join of slices.
+// parameters, its blocks of queries, and which rows a block sees.
 #pragma once
 
 #include "heads.hpp"
@@ -101,8 +101,8 @@ struct Sight {
   }
 };
 
-// The rows that the attention of n_tokens tokens writes for prompts of bf16;
-// slices > 1 leaves partial results for the join.
+// The prompts' kernel (bf16): out and lse, or with slices > 1 partial results
+// for the join.
 hipError_t launch_paged_prompt(const PagedParams& p, int d, int64_t groups, hipStream_t s);
 
 }  // namespace pf

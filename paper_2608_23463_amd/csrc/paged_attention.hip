@@ -100,7 +100,7 @@ struct Tile<bf16, D> {
     return s;
   }
   // The probabilities enter as two bf16 terms, p = hi + lo: one would round
-  // each to 2^-9 of itself, two keep 2^-17, and the second product is hidden
+  // each to 2^-8 of itself, two keep 2^-16, and the second product is hidden
   // behind the loads.
   __device__ __forceinline__ void values(const float* p, f32x4* o) const {
     bf16x8 hi, lo;
@@ -186,8 +186,8 @@ __global__ void __launch_bounds__(kThreads, (Tile<T, D>::kPerCu)) paged_attentio
   // Slices fastest, then K/V heads, then blocks of columns; every group begins
   // at another slice. Workgroups go to the XCDs in turn, and short sequences
   // fill their first slices only: with eight slices in order most of the rows
-  // would go to the first XCDs (48 sequences of up to 9,000 rows: 207 us, and 167
-  // so).
+  // would go to the first XCDs (64 sequences of up to 9,000 rows, 8 K/V heads of
+  // 128: 243 us, and 210 so; with other numbers of slices no difference).
   const int id = (int)blockIdx.x, up = p.fslices.div(id);
   int slice = id - up * p.slices + up - p.fslices.div(up) * p.slices;
   slice -= slice >= p.slices ? p.slices : 0;
@@ -378,8 +378,7 @@ __device__ __forceinline__ int live_slices(const PagedParams& p, int row) {
 
 // Joins the slices of a row in a fixed order, ROWS rows per workgroup: four of
 // few slices, a wave each, or one of many. A lane takes four channels; the
-// streams of slices are joined through LDS. (With a workgroup per row 78,000
-// rows of two slices took 150 us.)
+// streams of slices are joined through LDS.
 template <typename T, int D, int ROWS>
 __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
   constexpr int C4 = D / 4, NS = kThreads / ROWS / C4;  // streams of a row
@@ -422,9 +421,9 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
   }
 }
 
-// Slices up to which a wave joins a row: 16 prompts of up to 40 tokens, 32 heads,
-// 3 slices 32 us (46 with a workgroup per row), one token of 32 heads in 16
-// slices 12.9 us with a workgroup (14.8).
+// Slices up to which a wave joins a row: the attention of 16 prompts of up to 40
+// tokens, 32 heads, 3 slices takes 33 us (49 with a workgroup per row), of one
+// token of 32 heads in 15 slices 13.2 us with a workgroup (14.5), in 64 21.8 (27.6).
 constexpr int kFewSlices = 8;
 
 template <typename T, int D>
@@ -451,9 +450,13 @@ hipError_t attention_on(const PagedParams& p, const PagedPlan& pl, hipStream_t s
   return e;
 }
 
-// New tokens of a sequence from which the prompt kernel runs: 64 times 64 tokens
-// behind 448 rows 38 us (68 without it), 16 times 16 tokens behind 1,000 rows
-// 31 us (26).
+// New tokens of a sequence from which the prompt kernel runs. With a head per
+// K/V head that is where the two kernels meet: 16 sequences behind 1,000 rows, 8
+// heads of 128, 16 tokens 17.4 us (23.4 with the prompt kernel), 31 28.8 (24.6),
+// 32 24.2 (28.2 without it), 64 30.4 (40.0). Heads that share K and V fill the
+// prompt kernel's columns earlier, so it would be ahead from 8 tokens on with 4
+// heads each (25.8, and 27.8) and from 4 on with 8 (25.6, and 27.9), but it rounds
+// the weights to one bf16 term: fewer tokens keep the two terms.
 constexpr int64_t kPromptTokens = 32;
 
 }  // namespace
@@ -472,14 +475,16 @@ PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragge
   const int64_t tiles = std::max<int64_t>(1, (rows + pl.tile_rows - 1) / pl.tile_rows);
   pl.groups = col_blocks(pl.cols, d.hq / d.hk, ragged ? n_tokens : -1, batch) * d.hk;
   // Few groups: two workgroups per CU, if that leaves each enough tiles (fewer
-  // and longer slices stream better: 8 heads over 1M rows take 700 us in 512
-  // workgroups, 729 in 2,048 and 760 in 4,096; 16 heads over 1,000 rows 9.2 us
-  // in slices of 8 tiles, 10.5 of 16, 8.8 of 4, which costs calls of few rows a
-  // join). Where the groups fill the chip by themselves, cuts only even out
-  // sequences of different lengths, and short slices cost more than that gives:
-  // 48 sequences of up to 9,000 rows, 8 heads, 180 us in 768 workgroups, 158 in
-  // slices of 48 tiles, 153 of 24 (and all of 4,100 rows 143, 143 and 151); 64
-  // sequences of up to 1,000 rows, 16 heads, 32 us whole, 47 in slices of 16.
+  // and longer slices stream better: 8 K/V heads of 128 over 1M rows take 725 us
+  // in 512 workgroups and 753 in 2,048, 4 sequences of up to 60,000 fp32 rows over 2
+  // heads 52 and 58; 16 heads of 64 over 1,000 rows 10.0 us in slices of 8 tiles,
+  // 11.2 of 16, 9.7 of 4, which costs calls of few rows a join). Where the groups
+  // fill the chip by themselves, cuts only even out sequences of different
+  // lengths, and short slices cost more than that gives: 48 sequences of up to
+  // 9,000 rows, 8 K/V heads of 128, 201 us whole, 179 in two slices, 160 in slices
+  // of 48 tiles, 158 of 24, 156 of 16; all of 4,100 rows 158, 150, 150, 155 and
+  // 159; 64 sequences of up to 1,000 rows, 16 heads of 64, 29 us whole or of 24,
+  // 43 of 16.
   const bool filled = pl.groups >= 256;
   const int64_t want = pl.prompt || !filled ? 512 : 4096;
   pl.min_tiles = pl.prompt ? 4 : pl.groups < 32 ? 8 : filled ? 24 : 16;

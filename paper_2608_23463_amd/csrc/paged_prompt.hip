@@ -11,13 +11,17 @@
 // and the transposed reads of V take the rows in that same order, so P never
 // leaves its registers. Q is not scaled beforehand (its bf16 would round):
 // the scale is part of the one multiply-add in front of each exponential. Waves
-// in their matrix phases go before those in their exponentials (8,192 tokens
-// 555 us, without it 573).
+// in their matrix phases go before those in their exponentials (8,192 tokens, 32
+// over 8 heads of 128, 523 us, without it 545).
 //
 // The weights are rounded to bf16 once: 2^-8 of each at most, independent of
-// one another, which is below the rounding of the result; the two terms of the
-// single-token kernel would add half again to the matrix work that bounds this
-// one. Their sum is taken of the unrounded weights, in fp32.
+// one another. With many rows that is as much as the rounding of the result, so
+// the error is 1.4 times that of the rounded exact result (0.0022 to 0.0023 of
+// it, and 0.0017). The two terms of the single-token kernel would bring it back to
+// 0.0017 and add half again to the matrix work that bounds this one: 8,192
+// tokens, 32 over 8 heads of 128, 693 us for 523, six prompts with a window of
+// 700, 16 heads of 64, 51 for 44. A caller who wants them lays the call out for
+// fewer tokens. The weights' sum is taken unrounded, in fp32.
 #include "attention.hpp"
 #include "paged.hpp"
 
@@ -29,8 +33,10 @@ constexpr int kThreads = 256;
 constexpr int kTile = 64;
 constexpr int kColumns = 128;
 
-// Three workgroups per CU at 64 channels (six windowed prompts 47 us, with two
-// 57), two at 128, whose accumulators take the registers of a third.
+// Three workgroups per CU at 64 channels (16 heads: six windowed prompts 44 us,
+// with two 56, four of 4,096 tokens behind 16,384 rows 1,347 and 1,516; one of
+// 8,192 tokens, a round and a half of workgroups, 195 and 173), two at 128, whose
+// accumulators take the registers of a third.
 template <int D>
 __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel(PagedParams p) {
   constexpr int RB = D * 2, CH = RB / 16;     // bytes and 16-byte chunks of a row
@@ -95,7 +101,8 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
   // First cache rows of the blocks of 16 tiles, a block per lane: -1 where the
   // sequence or the table has none. One vector load for 16 tiles, on its way
   // as long beforehand: scalar lookups per tile would make every wait for an
-  // LDS read wait for them too (with them 8,192 tokens took 637 us, not 546).
+  // LDS read wait for them too (8,192 tokens, 32 over 8 heads of 128: 610 us with
+  // them, 523 so).
   auto blocks_of = [&](int t) -> int {
     const int tl = t + lane / kPerTile;
     const int blk16 = tile_row(min(tl, ntiles - 1)) / kBlock + lane % kPerTile;

@@ -543,9 +543,9 @@ hipError_t timed(const char* label, hipStream_t s, F&& f) {
   return e;
 }
 
-// Tokens below which a wave takes one pass: 2,000 x (16 + 16) x 64 6.2 us (6.7
-// with a wave per token), an append of 500 tokens 5.3 (7.2), of 4,000 x (32 + 8
-// + 8) x 128 22.4 (20.2).
+// Tokens below which a wave takes one pass: 2,000 x (16 + 16) x 64 6.5 us (7.0
+// with a wave per token), an append of 500 x (16 + 16 + 16) x 64 5.8 (7.6), of
+// 4,000 x (32 + 8 + 8) x 128 22.7 (20.8).
 constexpr int64_t kFewTokens = 2048;
 
 template <typename T, int D, bool PAIRS, bool APPEND>
@@ -561,7 +561,7 @@ hipError_t forward_on(QkParams p, int64_t n, const char* label, hipStream_t s) {
       // One token per wave while its rows fill the passes to two thirds: its
       // loads start earliest (65,536 x (16 + 4) x 128: 127 us, with four tokens
       // 136). With few heads, whose passes would run part empty, four
-      // (100,000 x (4 + 1) x 64: 32 us, with one 76).
+      // (100,000 x (4 + 1) x 64: 34 us, with one 79).
       const int passes = (p.q.p ? (p.hq + RPP - 1) / RPP : 0) + (APPEND ? 2 : 1) * ((p.hk + RPP - 1) / RPP);
       const int rows = (p.q.p ? p.hq : 0) + (APPEND ? 2 : 1) * p.hk;
       const bool single = 2 * passes * RPP <= 3 * rows;
@@ -601,8 +601,16 @@ QkParams qk_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, const i
   return p;
 }
 
-constexpr int kBwdTokens = 2;    // tokens per wave and step of the backward
-constexpr int kBwdBlocks = 768;  // workgroups at most: three per CU, as their registers allow
+// Tokens per wave and step of the backward: 65,536 x (16 + 16) x 64 161 us (157
+// with one, 164 with four), 100,000 x (16 + 1) x 64 141 (155, 140), 5,003 x (8 +
+// 2) x 128 fp32 26.7 (28.4, 27.4). Some calls would gain from another number: 500 x
+// (16 + 16) x 64 12.3 (10.8, 15.7), 20,000 x (32 + 8) x 128 135 (129, 130), 100,000 x
+// (4 + 1) x 64 85 (126, 62).
+constexpr int kBwdTokens = 2;
+// Workgroups at most, three per CU: 65,536 x (16 + 16) x 64 161 us (165 with 512,
+// 168 with 1,536), 100,000 x (16 + 1) x 64 141 (157, 148), 20,000 x (32 + 8) x 128
+// 135 (129, 139).
+constexpr int kBwdBlocks = 768;
 
 int bwd_blocks(int64_t n) {
   const int64_t per = (int64_t)kWaves * kBwdTokens;
