@@ -500,26 +500,30 @@ __global__ void __launch_bounds__(kThreads, 3) qk_backward_kernel(QkBwdParams p)
   }
 }
 
-// dgamma[w][c] = sum over the workgroups' rows, in a fixed order: 64 columns
-// per workgroup, 16 streams of rows joined through LDS, eight loads in flight
-// in each.
+// dgamma[w][c] = sum over the workgroups' rows, in a fixed order and 64 bits: 64
+// columns per workgroup, 16 streams of rows joined through LDS, eight loads in
+// flight in each (past the end the last row again: behind a condition each load
+// would be waited for by itself).
 __global__ void __launch_bounds__(1024) qk_gain_kernel(const float* part, int blocks, int D, float* dgq, float* dgk) {
-  __shared__ float sums[16][64];
+  __shared__ double sums[16][64];
   const int w = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 63), st = threadIdx.x >> 6;
   const float* p = part + (int64_t)w * blocks * D + c;
-  float v[8] = {};
+  double v[8] = {};
   for (int b = st; b < blocks; b += 16 * 8) {
+    float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += b + 16 * i < blocks ? p[(int64_t)(b + 16 * i) * D] : 0.0f;
+    for (int i = 0; i < 8; ++i) x[i] = p[(int64_t)min(b + 16 * i, blocks - 1) * D];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += b + 16 * i < blocks ? (double)x[i] : 0.0;
   }
   sums[st][threadIdx.x & 63] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   __syncthreads();
   if (st == 0) {
-    float all = 0.0f;
+    double all = 0.0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) all += sums[i][threadIdx.x];
     float* out = w ? dgk : dgq;
-    if (out) out[c] = all;
+    if (out) out[c] = (float)all;
   }
 }
 
