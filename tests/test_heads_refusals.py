@@ -28,7 +28,7 @@ def backward_with(w, dq=None, dk=None, pos=P):
 
 
 def test_rows_on_positions():
-    for pos in (FAR, FAR + 16, FAR + 2048):  # the rows end 3072 bytes on, or later
+    for pos in (FAR, FAR + 16, FAR + 2048):  # the rows end 3 KB on, or later
         refused(forward(pos=pos, qo=rows(FAR)))
         refused(forward(pos=pos, ko=rows(FAR)))
         refused(backward(pos=pos, dq=rows(FAR)))
