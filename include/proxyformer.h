@@ -496,6 +496,86 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
                           int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace,
                           size_t ws_bytes, void* stream);
 
+/* A cache of 8 bits in pages. k_pages and v_pages of `pages` hold e4m3 codes
+ * (the OCP 8-bit format with four exponent bits), one byte per element, and
+ * k_scales, v_scales [n_pages, n_kv_heads, page_size] a byte s for every row of
+ * a head: an element stands for code * 2^(s - 127). Everything else is as in
+ * pf_paged_cache; the bytes that rows are read with lie in 1..254. */
+typedef struct {
+  pf_paged_cache pages;
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+} pf_paged_quant_cache;
+
+/* New tokens into it, as proxy_paged_append. A row x, normed and turned in
+ * fp32, is held with the smallest s of 17..247 with max |x| <= 448 * 2^(s - 127),
+ * the largest over its finite elements, and each element as x * 2^(127 - s)
+ * rounded to e4m3, to nearest even: off by at most 2^-4 of itself, or 2^-10
+ * times the row's power of two where that is more. What is not finite is held
+ * as NaN. Magnitudes of 248 * 2^120 and more are read back as infinity. */
+int proxy_paged_quant_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_quant_cache* cache,
+                        int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
+                        const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream);
+
+/* What rows of it stand for, in the config's dtype (exact in both): those rows
+ * that an append of the same n_tokens and cu_tokens writes, into k_out and
+ * v_out [n_tokens, n_kv_heads] rows. Tokens without a place are left alone.
+ * With cu_tokens the running sums of kv_len these are the whole sequences.
+ * k_out and v_out overlap nothing else of the call. */
+int proxy_paged_quant_read(const pf_heads_config* cfg, const pf_paged_quant_cache* cache, int64_t n_tokens,
+                      const int32_t* cu_tokens, const pf_rows* k_out, const pf_rows* v_out, void* stream);
+
+/* Attention of new tokens over it, as proxy_paged_attention over what its rows
+ * stand for (workspace: proxy_paged_quant_workspace_size bytes). */
+size_t proxy_paged_quant_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
+                                   int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks);
+int proxy_paged_quant_attention(const pf_heads_config* cfg, const pf_paged_quant_cache* cache, int64_t n_tokens,
+                           const int32_t* cu_tokens, const pf_rows* q, int64_t max_new, int64_t max_kv_len,
+                           int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace,
+                           size_t ws_bytes, void* stream);
+
+/* Causal attention over whole sequences that lie one after another, in
+ * training (or for prompts whose cache is written aside).
+ *  cu_tokens int32 [batch + 1] (device), rising from 0: tokens cu_tokens[b] ..
+ *  cu_tokens[b + 1] - 1 are sequence b (empty ones are allowed), the i-th of
+ *  them its row i. It sees its sequence's rows up to i: all of them, or with
+ *  window > 0 the last `window` and the first `sinks` (ignored where window is
+ *  0), as in the paged attention.
+ *  q [n_tokens, n_heads], k, v [n_tokens, n_kv_heads] rows, already normed and
+ *  turned (cfg's norm and rotation are not applied here); tokens of k and v
+ *  (in the backward of q and dout too) at most 2^24 bytes apart.
+ *  max_len (at least 1): most tokens of a sequence, which the launch is laid out
+ *  for; longer ones are right but slower.
+ *  out [n_tokens, n_heads, head_dim] contiguous; lse fp32 [n_tokens, n_heads]:
+ *  log of the sum of exp(scale * q.k).
+ * Tokens behind the last sequence are left as they were. A row that a token
+ * does not see has no weight in its result; of the rows that other tokens of
+ * its tile see it is taken times zero, so an infinity or a NaN in one of those
+ * can reach it. Other sequences' rows cannot. In bf16 the weights are rounded
+ * to bf16 in their product with the values (their sum before that).
+ * n_tokens * n_heads below 2^31, n_tokens * n_heads / 128 + batch * n_kv_heads
+ * below 2^24; n_tokens = 0 does nothing. out and lse overlap nothing else of
+ * the call. The result is the same in every run. */
+int proxy_packed_attention_forward(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, const int32_t* cu_tokens,
+                                   const pf_rows* q, const pf_rows* k, const pf_rows* v, int64_t max_len,
+                                   int64_t window, int64_t sinks, float scale, void* out, float* lse, void* stream);
+
+/* Its backward: dq, dk and dv (rows) of q, k and v from dout (rows) and the
+ * forward's out and lse; dk and dv are summed over the query heads that share
+ * a key/value head. Every gradient is summed in fp32 in a fixed order and
+ * rounded once; in bf16 the weights and the scores' gradients are rounded to
+ * bf16 in their products. Tokens behind the last sequence are left as they
+ * were. dq, dk and dv overlap neither each other nor what the call reads; they
+ * may be bands of one buffer. workspace: proxy_packed_workspace_size bytes
+ * (0 for invalid sizes), 16-byte aligned, overlapping nothing else; calls that
+ * may run at the same time need workspaces of their own. */
+size_t proxy_packed_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens);
+int proxy_packed_attention_backward(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens,
+                                    const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k, const pf_rows* v,
+                                    int64_t max_len, int64_t window, int64_t sinks, float scale, const void* out,
+                                    const float* lse, const pf_rows* dout, const pf_rows* dq, const pf_rows* dk, const pf_rows* dv,
+                                    void* workspace, size_t ws_bytes, void* stream);
+
 /* Launch tracing (profiling aid). While enabled, every kernel launch of the
  * library is bracketed by two HIP events recorded on its stream and
  * attributed to a label (e.g. "gate_gemm", "attention_fwd", "decode_attn").

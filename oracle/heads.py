@@ -125,3 +125,83 @@ def paged_attention(q, k_pages, v_pages, table, kv_len, cu_tokens, scale, window
             out[t, h], mag[t, h] = p @ v, p @ np.abs(v)
             err[t, h] = abs(scale) * (np.abs(k) @ np.abs(q[t, h])).max()
     return out, lse, err, mag
+
+
+def packed_attention(q, k, v, cu, scale, window=0, sinks=0):
+    """(out, lse, score error scale, value magnitude) of whole sequences one
+    after another, q [T, Hq, D], k, v [T, Hk, D]; tokens behind the last
+    sequence are NaN. The last two as in paged_attention."""
+    q, k, v = (np.asarray(x, dtype=np.float64) for x in (q, k, v))
+    out, mag = np.full(q.shape, np.nan), np.full(q.shape, np.nan)
+    lse, err = np.full(q.shape[:2], np.nan), np.full(q.shape[:2], np.nan)
+    for a, b, h, hk in _sequence_heads(cu, q.shape[1], k.shape[1]):
+        p, lse[a:b, h] = _weights(q[a:b, h], k[a:b, hk], scale, window, sinks)
+        out[a:b, h], mag[a:b, h] = p @ v[a:b, hk], p @ np.abs(v[a:b, hk])
+        terms = abs(scale) * (np.abs(q[a:b, h]) @ np.abs(k[a:b, hk]).T)
+        err[a:b, h] = np.where(_mask(b - a, window, sinks), terms, 0).max(-1)
+    return out, lse, err, mag
+
+
+def _sequence_heads(cu, hq, hk):
+    for a, b in zip(cu[:-1], cu[1:]):
+        for h in range(hq if b > a else 0):
+            yield int(a), int(b), h, h * hk // hq
+
+
+def _mask(n, window, sinks):
+    return np.stack([visible(i, n, window, sinks) for i in range(n)])
+
+
+def _weights(q, k, scale, window, sinks):
+    s = np.where(_mask(len(q), window, sinks), scale * (q @ k.T), -np.inf)
+    top = s.max(-1, keepdims=True)
+    e = np.exp(s - top)
+    return e / e.sum(-1, keepdims=True), (top + np.log(e.sum(-1, keepdims=True)))[:, 0]
+
+
+def packed_attention_backward(q, k, v, dout, cu, scale, window=0, sinks=0, out_err=None, weight_err=None, term_err=0.0,
+                              product_err=0.0):
+    """((dq, dk, dv), (bound of each)). The bounds are those of an
+    implementation whose result `out` is off by out_err [T, Hq, D], whose
+    weights are off by weight_err [T, Hq] of themselves, which rounds weights
+    and the scores' gradients by term_err of themselves in their products and
+    forms products of D terms to product_err of the sum of their magnitudes."""
+    q, k, v, dout = (np.asarray(x, dtype=np.float64) for x in (q, k, v, dout))
+    grads, bounds = [[np.zeros(x.shape) for x in (q, k, v)] for _ in range(2)]
+    for a, b, h, hk in _sequence_heads(cu, q.shape[1], k.shape[1]):
+        qi, ki, vi, do = q[a:b, h], k[a:b, hk], v[a:b, hk], dout[a:b, h]
+        p, _ = _weights(qi, ki, scale, window, sinks)
+        dp = do @ vi.T
+        delta = (p * dp).sum(-1, keepdims=True)
+        ds = p * (dp - delta)
+        grads[0][a:b, h] = scale * (ds @ ki)
+        grads[1][a:b, hk] += scale * (ds.T @ qi)
+        grads[2][a:b, hk] += p.T @ do
+        if out_err is None:
+            continue
+        wide = np.abs(do) @ np.abs(vi).T  # magnitudes behind dp
+        w = weight_err[a:b, h][:, None]
+        o = p @ vi
+        off = (np.abs(do) * (out_err[a:b, h] + product_err * np.abs(o))).sum(-1, keepdims=True)  # of delta
+        e = p * (w * np.abs(dp - delta) + product_err * wide + off) * (1 + w) * (1 + term_err) + term_err * np.abs(ds)
+        e += product_err * np.abs(ds)  # their sums
+        bounds[0][a:b, h] = abs(scale) * (e @ np.abs(ki))
+        bounds[1][a:b, hk] += abs(scale) * (e.T @ np.abs(qi))
+        bounds[2][a:b, hk] += ((w + term_err + w * term_err + product_err) * p).T @ np.abs(do)
+    return grads, bounds
+
+
+def quantised(x):
+    """(values, scale bytes) of rows x [..., D] held in 8 bits: x / 2^e rounded to
+    e4m3 (three bits behind the first, 2^-9 at the least, ties to even), e the
+    smallest of -110.. that takes the row's largest finite magnitude to at most
+    448; what is not finite is NaN. Values are codes times 2^e."""
+    x = np.asarray(x, dtype=np.float64)
+    top = np.where(np.isfinite(x), np.abs(x), 0).max(-1)
+    e = np.full(top.shape, -110)
+    while (grow := top > 448 * np.exp2(e.astype(np.float64))).any():
+        e += grow
+    scale = np.exp2(e.astype(np.float64))[..., None]
+    y = x / scale
+    step = np.exp2(np.maximum(np.floor(np.log2(np.maximum(np.abs(np.where(np.isfinite(y), y, 1)), 2.0 ** -30))), -6) - 3)
+    return np.where(np.isfinite(x), np.rint(y / step) * step * scale, np.nan), (e + 127).astype(np.uint8)

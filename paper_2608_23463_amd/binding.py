@@ -45,6 +45,8 @@ EXPORTS = (
     "proxy_ceiling_mfma", "proxy_decode_step_static", "proxy_ceiling_read",
     "proxy_qk_norm_rope_forward", "proxy_qk_workspace_size", "proxy_qk_norm_rope_backward",
     "proxy_paged_append", "proxy_paged_workspace_size", "proxy_paged_attention",
+    "proxy_paged_quant_append", "proxy_paged_quant_read", "proxy_paged_quant_workspace_size", "proxy_paged_quant_attention",
+    "proxy_packed_attention_forward", "proxy_packed_workspace_size", "proxy_packed_attention_backward",
 )
 
 c_void_p = ctypes.c_void_p
@@ -115,6 +117,10 @@ class PfRows(ctypes.Structure):
 class PfPagedCache(ctypes.Structure):
     _fields_ = [("k_pages", c_void_p), ("v_pages", c_void_p), ("n_pages", c_int32), ("page_size", c_int32),
                 ("page_table", c_void_p), ("max_pages", c_int32), ("kv_len", c_void_p), ("batch", c_int32)]
+
+
+class PfPagedQuantCache(ctypes.Structure):
+    _fields_ = [("pages", PfPagedCache), ("k_scales", c_void_p), ("v_scales", c_void_p)]
 
 
 _lib = None
@@ -242,6 +248,24 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                           c_int64, c_int64, ctypes.c_float, c_void_p, c_void_p, c_void_p, c_size_t,
                                           c_void_p]
     lib.proxy_paged_attention.restype = c_int32
+    lib.proxy_paged_quant_append.argtypes = [P(PfHeadsConfig), P(PfHeadsWeights), P(PfPagedQuantCache), c_int64, c_void_p, rows,
+                                        rows, rows, c_void_p, rows, c_void_p]
+    lib.proxy_paged_quant_append.restype = c_int32
+    lib.proxy_paged_quant_read.argtypes = [P(PfHeadsConfig), P(PfPagedQuantCache), c_int64, c_void_p, rows, rows, c_void_p]
+    lib.proxy_paged_quant_read.restype = c_int32
+    lib.proxy_paged_quant_workspace_size.argtypes = lib.proxy_paged_workspace_size.argtypes
+    lib.proxy_paged_quant_workspace_size.restype = c_size_t
+    lib.proxy_paged_quant_attention.argtypes = [P(PfHeadsConfig), P(PfPagedQuantCache), *lib.proxy_paged_attention.argtypes[2:]]
+    lib.proxy_paged_quant_attention.restype = c_int32
+    lib.proxy_packed_attention_forward.argtypes = [P(PfHeadsConfig), c_int32, c_int64, c_void_p, rows, rows, rows, c_int64,
+                                                   c_int64, c_int64, ctypes.c_float, c_void_p, c_void_p, c_void_p]
+    lib.proxy_packed_attention_forward.restype = c_int32
+    lib.proxy_packed_workspace_size.argtypes = [P(PfHeadsConfig), c_int32, c_int64]
+    lib.proxy_packed_workspace_size.restype = c_size_t
+    lib.proxy_packed_attention_backward.argtypes = [P(PfHeadsConfig), c_int32, c_int64, c_void_p, rows, rows, rows, c_int64,
+                                                    c_int64, c_int64, ctypes.c_float, c_void_p, c_void_p, rows, rows, rows,
+                                                    rows, c_void_p, c_size_t, c_void_p]
+    lib.proxy_packed_attention_backward.restype = c_int32
     _lib = lib
     return lib
 
@@ -741,6 +765,74 @@ def qk_norm_rope_backward(cfg: PfHeadsConfig, weights: Dict[str, object], q, k, 
     return dq, dk, gq, gk
 
 
+def packed_attention_forward(cfg: PfHeadsConfig, q, k, v, cu_tokens, max_len: int, window: int = 0, sinks: int = 0,
+                             scale: Optional[float] = None, out=None, lse=None, stream=None):
+    """Causal attention over whole sequences that lie one after another:
+    q [T, n_heads, head_dim], k, v [T, n_kv_heads, head_dim], normed and turned
+    beforehand; cu_tokens int32 [batch + 1] on the device: sequence b is tokens
+    cu_tokens[b] .. cu_tokens[b + 1] - 1. window > 0: a token sees the last
+    `window` rows of its sequence and the first `sinks`. max_len: most tokens
+    of a sequence, to lay the launch out for. scale: 1 / sqrt(head_dim) unless
+    given. Returns (out, lse), lse fp32 [T, n_heads]; rows of tokens behind the
+    last sequence are left alone."""
+    import torch
+    dev, n = q.device, q.shape[0]
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return packed_attention_forward(cfg, q, k, v, cu_tokens, max_len, window, sinks, scale, out, lse)
+    rq = _rows(cfg, "q", q, n, cfg.n_heads, dev)
+    rk, rv = _rows(cfg, "k", k, n, cfg.n_kv_heads, dev), _rows(cfg, "v", v, n, cfg.n_kv_heads, dev)
+    cu = _want("cu_tokens", cu_tokens, torch.int32, dev, (None,))
+    shape = (n, cfg.n_heads, cfg.head_dim)
+    if out is None:
+        out = _empty(shape, q.dtype, dev)
+    if lse is None:
+        lse = _empty(shape[:2], torch.float32, dev)
+    to, tl = _want("out", out, q.dtype, dev, shape), _want("lse", lse, torch.float32, dev, shape[:2])
+    _check(load().proxy_packed_attention_forward(cfg, cu_tokens.shape[0] - 1, n, cu, rq, rk, rv, max_len, window, sinks,
+                                                 cfg.head_dim ** -0.5 if scale is None else scale, to, tl, _current(dev)))
+    return out, lse
+
+
+def packed_attention_backward(cfg: PfHeadsConfig, q, k, v, out, lse, dout, cu_tokens, max_len: int, window: int = 0,
+                              sinks: int = 0, scale: Optional[float] = None, dq=None, dk=None, dv=None, workspace=None,
+                              stream=None):
+    """Gradients (dq, dk, dv) of packed_attention_forward's q, k and v from
+    dout [T, n_heads, head_dim], with that call's inputs and results. workspace:
+    a byte tensor that no call running at the same time uses (allocated unless
+    given)."""
+    import torch
+    dev, n = q.device, q.shape[0]
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return packed_attention_backward(cfg, q, k, v, out, lse, dout, cu_tokens, max_len, window, sinks, scale, dq, dk,
+                                             dv, workspace)
+    lib = load()
+    hq, hk = cfg.n_heads, cfg.n_kv_heads
+    rq, rk, rv = _rows(cfg, "q", q, n, hq, dev), _rows(cfg, "k", k, n, hk, dev), _rows(cfg, "v", v, n, hk, dev)
+    ro = _rows(cfg, "dout", dout, n, hq, dev)
+    cu = _want("cu_tokens", cu_tokens, torch.int32, dev, (None,))
+    batch = cu_tokens.shape[0] - 1
+    to = _want("out", out, q.dtype, dev, (n, hq, cfg.head_dim))
+    tl = _want("lse", lse, torch.float32, dev, (n, hq))
+    if dq is None:
+        dq = _empty((n, hq, cfg.head_dim), q.dtype, dev)
+    if dk is None:
+        dk = _empty((n, hk, cfg.head_dim), q.dtype, dev)
+    if dv is None:
+        dv = _empty((n, hk, cfg.head_dim), q.dtype, dev)
+    wq, wk, wv = _rows(cfg, "dq", dq, n, hq, dev), _rows(cfg, "dk", dk, n, hk, dev), _rows(cfg, "dv", dv, n, hk, dev)
+    if workspace is None:
+        workspace = _bytes(int(lib.proxy_packed_workspace_size(cfg, batch, n)), dev)
+    ws, ws_bytes = _workspace(workspace, dev)
+    _check(lib.proxy_packed_attention_backward(cfg, batch, n, cu, rq, rk, rv, max_len, window, sinks,
+                                               cfg.head_dim ** -0.5 if scale is None else scale, to, tl, ro, wq, wk, wv, ws,
+                                               ws_bytes, _current(dev)))
+    return dq, dk, dv
+
+
 class PagedCache:
     """A cache of the fine tokens' keys and values in pages (one per layer).
 
@@ -751,9 +843,11 @@ class PagedCache:
     cfg and weights are taken as they are when the cache is made: later changes
     of the config or of the dict's entries do not reach it."""
 
+    _calls = "proxy_paged_append", "proxy_paged_workspace_size", "proxy_paged_attention"
+
     def __init__(self, cfg: PfHeadsConfig, weights: Dict[str, object], k_pages, v_pages, page_table, kv_len):
         import torch
-        dev, dt = k_pages.device, _heads_dtype(cfg)
+        dev, dt = k_pages.device, self._page_dtype(cfg)
         if dev.type != "cuda":
             raise ValueError(f"tensors must be on a GPU, got {dev}")
         shape = (k_pages.shape[0], cfg.n_kv_heads, None, cfg.head_dim)
@@ -768,6 +862,10 @@ class PagedCache:
                                   _want("v_pages", v_pages, dt, dev, tuple(k_pages.shape)), k_pages.shape[0],
                                   k_pages.shape[2], _want("page_table", page_table, torch.int32, dev, (batch, None)),
                                   page_table.shape[1], _want("kv_len", kv_len, torch.int32, dev, (batch,)), batch)
+
+    @staticmethod
+    def _page_dtype(cfg):
+        return _heads_dtype(cfg)
 
     def append(self, k, v, q=None, cu_tokens=None, positions=None, q_out=None, stream=None):
         """New tokens' keys and values [T, n_kv_heads, head_dim] into the pages,
@@ -793,7 +891,8 @@ class PagedCache:
             ro = _rows(cfg, "q_out", q_out, n, cfg.n_heads, dev)
         elif q_out is not None:
             raise ValueError("q_out without q")
-        _check(load().proxy_paged_append(cfg, self.wstruct, self.state, n, cu, rq, rk, rv, at, ro, _current(dev)))
+        call = getattr(load(), self._calls[0])
+        _check(call(cfg, self.wstruct, self.state, n, cu, rq, rk, rv, at, ro, _current(dev)))
         return q_out
 
     def attend(self, q, max_kv_len: int, cu_tokens=None, max_new: Optional[int] = None, window: int = 0,
@@ -826,10 +925,52 @@ class PagedCache:
         to = _want("out", out, q.dtype, dev, shape)
         tl = None if lse is None else _want("lse", lse, torch.float32, dev, (n, cfg.n_heads))
         if workspace is None:
-            need = lib.proxy_paged_workspace_size(cfg, self.batch, n, cu is not None, max_new, max_kv_len, window, sinks)
+            size = getattr(lib, self._calls[1])
+            need = size(cfg, self.batch, n, cu is not None, max_new, max_kv_len, window, sinks)
             workspace = _bytes(need, dev) if need else None
         ws, ws_bytes = _workspace(workspace, dev)
-        _check(lib.proxy_paged_attention(cfg, self.state, n, cu, rq, max_new, max_kv_len, window, sinks,
-                                         cfg.head_dim ** -0.5 if scale is None else scale, to, tl, ws, ws_bytes,
-                                         _current(dev)))
+        call = getattr(lib, self._calls[2])
+        _check(call(cfg, self.state, n, cu, rq, max_new, max_kv_len, window, sinks,
+                    cfg.head_dim ** -0.5 if scale is None else scale, to, tl, ws, ws_bytes, _current(dev)))
         return out
+
+
+class PagedCache8(PagedCache):
+    """A PagedCache whose pages hold 8 bits per element, half the bytes of bf16:
+    k_pages, v_pages torch.float8_e4m3fn, and a scale byte s for every row of a
+    head in k_scales, v_scales uint8 [n_pages, n_kv_heads, page_size]; an element
+    stands for code * 2 ** (s - 127). append rounds to it, attend takes the
+    values as they stand, read gives them back."""
+
+    _calls = "proxy_paged_quant_append", "proxy_paged_quant_workspace_size", "proxy_paged_quant_attention"
+
+    def __init__(self, cfg: PfHeadsConfig, weights: Dict[str, object], k_pages, v_pages, k_scales, v_scales, page_table,
+                 kv_len):
+        import torch
+        super().__init__(cfg, weights, k_pages, v_pages, page_table, kv_len)
+        shape = tuple(k_pages.shape[:3])
+        self.tensors += (k_scales, v_scales)
+        self.state = PfPagedQuantCache(self.state, _want("k_scales", k_scales, torch.uint8, self.device, shape),
+                                   _want("v_scales", v_scales, torch.uint8, self.device, shape))
+
+    @staticmethod
+    def _page_dtype(cfg):
+        import torch
+        return torch.float8_e4m3fn
+
+    def read(self, k_out, v_out, cu_tokens=None, stream=None):
+        """What the rows of the last tokens of every sequence stand for, into
+        k_out and v_out [T, n_kv_heads, head_dim] of the config's type: those
+        rows that an append with the same cu_tokens writes (None: the last of
+        every sequence; running sums of kv_len: all of them). Rows without a
+        place are left alone. Returns (k_out, v_out)."""
+        import torch
+        cfg, dev, n = self.cfg, self.device, k_out.shape[0]
+        ctx = _elsewhere(dev, stream)
+        if ctx is not None:
+            with ctx:
+                return self.read(k_out, v_out, cu_tokens)
+        rk, rv = _rows(cfg, "k_out", k_out, n, cfg.n_kv_heads, dev), _rows(cfg, "v_out", v_out, n, cfg.n_kv_heads, dev)
+        cu = None if cu_tokens is None else _want("cu_tokens", cu_tokens, torch.int32, dev, (self.batch + 1,))
+        _check(load().proxy_paged_quant_read(cfg, self.state, n, cu, rk, rv, _current(dev)))
+        return k_out, v_out

@@ -669,7 +669,8 @@ int proxy_qk_norm_rope_backward(const pf_heads_config* cfg, const pf_heads_weigh
                     "proxy_qk_norm_rope_backward launch");
 }
 
-static int check_paged(const pf_paged_cache* c, const HeadsDims& d, PagedDims* o) {
+// Pages of `esize` bytes per element.
+static int check_paged(const pf_paged_cache* c, const HeadsDims& d, int esize, PagedDims* o) {
   if (!c) return fail(PF_ERR_INVALID_ARG, "cache is NULL");
   if (!c->k_pages || !c->v_pages || !c->page_table || !c->kv_len)
     return fail(PF_ERR_INVALID_ARG, "k_pages, v_pages, page_table and kv_len must be non-NULL");
@@ -684,37 +685,60 @@ static int check_paged(const pf_paged_cache* c, const HeadsDims& d, PagedDims* o
     return fail(PF_ERR_UNSUPPORTED, "max_pages * page_size above 2^31 - 65536");
   if ((__int128)c->n_pages * d.hk * c->page_size > INT32_MAX)
     return fail(PF_ERR_UNSUPPORTED, "n_pages * n_kv_heads * page_size above 2^31 - 1");
-  const size_t bytes = (size_t)c->n_pages * d.hk * c->page_size * d.d * d.esize;
+  const size_t bytes = (size_t)c->n_pages * d.hk * c->page_size * d.d * esize;
   if (overlaps(c->k_pages, bytes, c->v_pages, bytes))
     return fail(PF_ERR_INVALID_ARG, "k_pages and v_pages must not overlap");
-  *o = PagedDims{static_cast<char*>(c->k_pages), static_cast<char*>(c->v_pages), c->n_pages, c->page_size,
-                 c->page_table, c->max_pages, c->kv_len, c->batch};
+  *o = PagedDims{static_cast<char*>(c->k_pages), static_cast<char*>(c->v_pages), nullptr, nullptr, c->n_pages,
+                 c->page_size, c->page_table, c->max_pages, c->kv_len, c->batch};
   return PF_OK;
 }
 
-int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_cache* cache,
-                       int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
-                       const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream) {
-  HeadsDims d;
-  HeadsWeights hw;
-  PagedDims c;
-  int st = check_heads(cfg, w, n_tokens, &d, &hw);
+static int check_paged_quant(const pf_paged_quant_cache* c, const HeadsDims& d, PagedDims* o) {
+  if (!c) return fail(PF_ERR_INVALID_ARG, "cache is NULL");
+  const int st = check_paged(&c->pages, d, 1, o);
   if (st != PF_OK) return st;
-  if ((st = check_paged(cache, d, &c)) != PF_OK) return st;
-  if (!cu_tokens && n_tokens != c.batch)
+  if (!c->k_scales || !c->v_scales) return fail(PF_ERR_INVALID_ARG, "k_scales and v_scales must be non-NULL");
+  if (!aligned16(c->k_scales) || !aligned16(c->v_scales))
+    return fail(PF_ERR_INVALID_ARG, "scales must be 16-byte aligned");
+  o->k_scale = c->k_scales;
+  o->v_scale = c->v_scales;
+  const size_t rows = (size_t)o->n_pages * d.hk * o->page_size;
+  const Extent e[4] = {{o->k, rows * d.d}, {o->v, rows * d.d}, {o->k_scale, rows}, {o->v_scale, rows}};
+  if (any_meet(e, 4, nullptr, 0)) return fail(PF_ERR_INVALID_ARG, "pages and scales must not overlap");
+  return PF_OK;
+}
+
+// What a cache's pages and scales take up (four extents, those of scales empty
+// where the pages are of the rows' type), and its table and lengths.
+struct CacheExtents {
+  Extent pages[4], tables[3];
+  CacheExtents(const PagedDims& c, const HeadsDims& d, const int32_t* cu) {
+    const size_t rows = (size_t)c.n_pages * d.hk * c.page_size, es = c.k_scale ? 1 : d.esize;
+    pages[0] = {c.k, rows * d.d * es};
+    pages[1] = {c.v, rows * d.d * es};
+    pages[2] = {c.k_scale, rows};
+    pages[3] = {c.v_scale, rows};
+    tables[0] = {c.table, (size_t)c.batch * c.max_pages * sizeof(int32_t)};
+    tables[1] = {c.kv_len, (size_t)c.batch * sizeof(int32_t)};
+    tables[2] = {cu, ((size_t)c.batch + 1) * sizeof(int32_t)};
+  }
+  bool meets_pages(const Extent& e) const { return any_meet(&e, 1, pages, 4); }
+};
+
+static int paged_append(const char* what, const HeadsDims& d, const HeadsWeights& hw, const PagedDims& c, int64_t n,
+                        const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k, const pf_rows* v,
+                        const int32_t* positions, const pf_rows* q_out, void* stream) {
+  int st;
+  if (!cu_tokens && n != c.batch)
     return fail(PF_ERR_INVALID_ARG, "without cu_tokens n_tokens must be batch: one token of every sequence");
   if (!aligned4(cu_tokens) || !aligned4(positions))
     return fail(PF_ERR_INVALID_ARG, "cu_tokens and positions must be 4-byte aligned");
-  if (n_tokens == 0) return PF_OK;
-  const int64_t n = n_tokens;
+  if (n == 0) return PF_OK;
   const bool with_q = q && q->p;
   if ((st = check_rows("k", k, n, d.hk, d, false)) != PF_OK) return st;
   if ((st = check_rows("v", v, n, d.hk, d, false)) != PF_OK) return st;
-  const size_t pages = (size_t)c.n_pages * d.hk * c.page_size * d.d * d.esize;
-  auto on_pages = [&](const pf_rows* r, int heads) {
-    const size_t bytes = rows_bytes(*r, n, heads, d);
-    return overlaps(r->p, bytes, c.k, pages) || overlaps(r->p, bytes, c.v, pages);
-  };
+  const CacheExtents held(c, d, cu_tokens);
+  auto on_pages = [&](const pf_rows* r, int heads) { return held.meets_pages(extent_of(r, n, heads, d)); };
   if (with_q) {
     if ((st = check_rows("q", q, n, d.hq, d, false)) != PF_OK) return st;
     if ((st = check_rows("q_out", q_out, n, d.hq, d, true)) != PF_OK) return st;
@@ -725,26 +749,125 @@ int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, co
   }
   if (on_pages(k, d.hk) || on_pages(v, d.hk)) return fail(PF_ERR_INVALID_ARG, "k and v must not overlap the pages");
   const SmallInputs small(d, hw, positions, n);
-  const Extent tables[3] = {{c.table, (size_t)c.batch * c.max_pages * sizeof(int32_t)},
-                            {c.kv_len, (size_t)c.batch * sizeof(int32_t)},
-                            {cu_tokens, ((size_t)c.batch + 1) * sizeof(int32_t)}};
-  for (const Extent& w : {with_q ? extent_of(q_out, n, d.hq, d) : Extent{nullptr, 0}, Extent{c.k, pages}, Extent{c.v, pages}})
-    if (small.meets(w) || any_meet(&w, 1, tables, 3))
+  for (const Extent& w : {with_q ? extent_of(q_out, n, d.hq, d) : Extent{nullptr, 0}, held.pages[0], held.pages[1],
+                          held.pages[2], held.pages[3]})
+    if (small.meets(w) || any_meet(&w, 1, held.tables, 3))
       return fail(PF_ERR_INVALID_ARG, "q_out and the pages must not overlap gains, freqs, positions, table or lengths");
   return hip_status(launch_paged_append(d, hw, c, n, cu_tokens, with_q ? rows_of(q) : Rows{}, rows_of(k), rows_of(v),
                                         positions, with_q ? rows_of(q_out) : Rows{},
                                         reinterpret_cast<hipStream_t>(stream)),
-                    "proxy_paged_append launch");
+                    what);
 }
 
-size_t proxy_paged_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
-                                  int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks) {
+int proxy_paged_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_cache* cache,
+                       int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
+                       const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream) {
+  HeadsDims d;
+  HeadsWeights hw;
+  PagedDims c;
+  int st = check_heads(cfg, w, n_tokens, &d, &hw);
+  if (st != PF_OK) return st;
+  if ((st = check_paged(cache, d, d.esize, &c)) != PF_OK) return st;
+  return paged_append("proxy_paged_append launch", d, hw, c, n_tokens, cu_tokens, q, k, v, positions, q_out, stream);
+}
+
+int proxy_paged_quant_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_quant_cache* cache,
+                        int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
+                        const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream) {
+  HeadsDims d;
+  HeadsWeights hw;
+  PagedDims c;
+  int st = check_heads(cfg, w, n_tokens, &d, &hw);
+  if (st != PF_OK) return st;
+  if ((st = check_paged_quant(cache, d, &c)) != PF_OK) return st;
+  return paged_append("proxy_paged_quant_append launch", d, hw, c, n_tokens, cu_tokens, q, k, v, positions, q_out, stream);
+}
+
+int proxy_paged_quant_read(const pf_heads_config* cfg, const pf_paged_quant_cache* cache, int64_t n_tokens,
+                      const int32_t* cu_tokens, const pf_rows* k_out, const pf_rows* v_out, void* stream) {
+  HeadsDims d;
+  PagedDims c;
+  const char* why;
+  int st = heads_dims(cfg, &d, &why);
+  if (st != PF_OK) return fail(st, "invalid heads config: %s", why);
+  if ((st = check_paged_quant(cache, d, &c)) != PF_OK) return st;
+  const int64_t n = n_tokens;
+  if (n < 0) return fail(PF_ERR_INVALID_ARG, "n_tokens must be >= 0");
+  if (n > kMaxTokens) return fail(PF_ERR_UNSUPPORTED, "n_tokens above %lld", (long long)kMaxTokens);
+  if (!cu_tokens && n != c.batch)
+    return fail(PF_ERR_INVALID_ARG, "without cu_tokens n_tokens must be batch: one token of every sequence");
+  if (!aligned4(cu_tokens)) return fail(PF_ERR_INVALID_ARG, "cu_tokens must be 4-byte aligned");
+  if (n == 0) return PF_OK;
+  if ((st = check_rows("k_out", k_out, n, d.hk, d, true)) != PF_OK) return st;
+  if ((st = check_rows("v_out", v_out, n, d.hk, d, true)) != PF_OK) return st;
+  if (rows_meet(*k_out, d.hk, *v_out, d.hk, n, d)) return fail(PF_ERR_INVALID_ARG, "k_out and v_out must not overlap");
+  const CacheExtents held(c, d, cu_tokens);
+  for (const pf_rows* r : {k_out, v_out}) {
+    const Extent e = extent_of(r, n, d.hk, d);
+    if (held.meets_pages(e) || any_meet(&e, 1, held.tables, 3))
+      return fail(PF_ERR_INVALID_ARG, "k_out and v_out must not overlap the pages, scales, table or lengths");
+  }
+  return hip_status(launch_paged_quant_read(d, c, n, cu_tokens, rows_of(k_out), rows_of(v_out),
+                                       reinterpret_cast<hipStream_t>(stream)),
+                    "proxy_paged_quant_read launch");
+}
+
+static size_t paged_workspace(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
+                              int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks, bool bits8) {
   HeadsDims d;
   const char* why;
   if (heads_dims(cfg, &d, &why) != PF_OK || batch < 1 || n_tokens < 1 || n_tokens > INT32_MAX || max_new < 1 ||
       max_kv_len < 1 || window < 0 || sinks < 0)
     return 0;
-  return paged_plan(d, batch, n_tokens, ragged != 0, max_new, max_kv_len, window, sinks).bytes;
+  return paged_plan(d, batch, n_tokens, ragged != 0, max_new, max_kv_len, window, sinks, bits8).bytes;
+}
+
+size_t proxy_paged_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
+                                  int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks) {
+  return paged_workspace(cfg, batch, n_tokens, ragged, max_new, max_kv_len, window, sinks, false);
+}
+
+size_t proxy_paged_quant_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
+                                   int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks) {
+  return paged_workspace(cfg, batch, n_tokens, ragged, max_new, max_kv_len, window, sinks, true);
+}
+
+static int paged_attention(const char* what, const HeadsDims& d, const PagedDims& c, int64_t n_tokens,
+                           const int32_t* cu_tokens, const pf_rows* q, int64_t max_new, int64_t max_kv_len,
+                           int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace,
+                           size_t ws_bytes, void* stream) {
+  int st;
+  if (n_tokens < 0) return fail(PF_ERR_INVALID_ARG, "n_tokens must be >= 0");
+  if (!cu_tokens && n_tokens != c.batch)
+    return fail(PF_ERR_INVALID_ARG, "without cu_tokens n_tokens must be batch: one token of every sequence");
+  if (!aligned4(cu_tokens)) return fail(PF_ERR_INVALID_ARG, "cu_tokens must be 4-byte aligned");
+  if (max_new < 1 || max_kv_len < 1) return fail(PF_ERR_INVALID_ARG, "max_new and max_kv_len must be >= 1");
+  if (window < 0 || sinks < 0) return fail(PF_ERR_INVALID_ARG, "window and sinks must be >= 0");
+  if (!(std::fabs(scale) < 2.3e38f)) return fail(PF_ERR_INVALID_ARG, "scale must be finite and below 2.3e38");
+  if (n_tokens == 0) return PF_OK;
+  if (n_tokens > INT32_MAX / d.hq) return fail(PF_ERR_UNSUPPORTED, "n_tokens * n_heads above 2^28");
+  const int64_t n = n_tokens;
+  const PagedPlan pl = paged_plan(d, c.batch, n, cu_tokens != nullptr, max_new, max_kv_len, window, sinks, c.k_scale != nullptr);
+  if (pl.groups > kMaxGroups / pl.slices)
+    return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes: n_tokens * n_heads / 16 + batch * n_kv_heads must stay below 2^24");
+  if ((st = check_rows("q", q, n, d.hq, d, false)) != PF_OK) return st;
+  if (!out) return fail(PF_ERR_INVALID_ARG, "out is NULL");
+  if (!aligned16(out)) return fail(PF_ERR_INVALID_ARG, "out must be 16-byte aligned");
+  if (!aligned4(lse)) return fail(PF_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+  if (pl.bytes && (!workspace || ws_bytes < pl.bytes))
+    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", pl.bytes, workspace ? ws_bytes : 0);
+  if (!aligned16(workspace)) return fail(PF_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  const CacheExtents held(c, d, cu_tokens);
+  const Extent wr[3] = {{out, (size_t)n * d.hq * d.d * d.esize},
+                        {lse, (size_t)n * d.hq * sizeof(float)},
+                        {workspace, pl.bytes}};
+  const Extent rd[8] = {extent_of(q, n, d.hq, d), held.pages[0],  held.pages[1],  held.pages[2],
+                        held.pages[3],            held.tables[0], held.tables[1], held.tables[2]};
+  if (any_meet(wr, 3, rd, 8))
+    return fail(PF_ERR_INVALID_ARG, "out, lse and workspace must not overlap other buffers of the call");
+  return hip_status(launch_paged_attention(d, c, pl, n, cu_tokens, rows_of(q), scale, window, sinks, out, lse,
+                                           static_cast<char*>(workspace), reinterpret_cast<hipStream_t>(stream)),
+                    what);
 }
 
 int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cache, int64_t n_tokens,
@@ -756,42 +879,129 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
   const char* why;
   int st = heads_dims(cfg, &d, &why);
   if (st != PF_OK) return fail(st, "invalid heads config: %s", why);
-  if ((st = check_paged(cache, d, &c)) != PF_OK) return st;
-  if (n_tokens < 0) return fail(PF_ERR_INVALID_ARG, "n_tokens must be >= 0");
-  if (!cu_tokens && n_tokens != c.batch)
-    return fail(PF_ERR_INVALID_ARG, "without cu_tokens n_tokens must be batch: one token of every sequence");
+  if ((st = check_paged(cache, d, d.esize, &c)) != PF_OK) return st;
+  return paged_attention("proxy_paged_attention launch", d, c, n_tokens, cu_tokens, q, max_new, max_kv_len, window, sinks,
+                         scale, out, lse, workspace, ws_bytes, stream);
+}
+
+int proxy_paged_quant_attention(const pf_heads_config* cfg, const pf_paged_quant_cache* cache, int64_t n_tokens,
+                           const int32_t* cu_tokens, const pf_rows* q, int64_t max_new, int64_t max_kv_len,
+                           int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace,
+                           size_t ws_bytes, void* stream) {
+  HeadsDims d;
+  PagedDims c;
+  const char* why;
+  int st = heads_dims(cfg, &d, &why);
+  if (st != PF_OK) return fail(st, "invalid heads config: %s", why);
+  if ((st = check_paged_quant(cache, d, &c)) != PF_OK) return st;
+  return paged_attention("proxy_paged_quant_attention launch", d, c, n_tokens, cu_tokens, q, max_new, max_kv_len, window, sinks,
+                         scale, out, lse, workspace, ws_bytes, stream);
+}
+
+// What the packed attention's two directions check alike. Rows lie within a
+// 32-bit offset of the first of a tile of 64.
+static int check_packed(const pf_heads_config* cfg, int32_t batch, int64_t n, const int32_t* cu_tokens, const pf_rows* q,
+                        const pf_rows* k, const pf_rows* v, int64_t max_len, int64_t window, int64_t sinks, float scale,
+                        const void* out, const float* lse, HeadsDims* d) {
+  const char* why;
+  int st = heads_dims(cfg, d, &why);
+  if (st != PF_OK) return fail(st, "invalid heads config: %s", why);
+  if (batch < 1) return fail(PF_ERR_INVALID_ARG, "batch must be >= 1");
+  if (n < 0) return fail(PF_ERR_INVALID_ARG, "n_tokens must be >= 0");
+  if (!cu_tokens) return fail(PF_ERR_INVALID_ARG, "cu_tokens is NULL");
   if (!aligned4(cu_tokens)) return fail(PF_ERR_INVALID_ARG, "cu_tokens must be 4-byte aligned");
-  if (max_new < 1 || max_kv_len < 1) return fail(PF_ERR_INVALID_ARG, "max_new and max_kv_len must be >= 1");
+  if (max_len < 1) return fail(PF_ERR_INVALID_ARG, "max_len must be >= 1");
   if (window < 0 || sinks < 0) return fail(PF_ERR_INVALID_ARG, "window and sinks must be >= 0");
   if (!(std::fabs(scale) < 2.3e38f)) return fail(PF_ERR_INVALID_ARG, "scale must be finite and below 2.3e38");
-  if (n_tokens == 0) return PF_OK;
-  if (n_tokens > INT32_MAX / d.hq) return fail(PF_ERR_UNSUPPORTED, "n_tokens * n_heads above 2^28");
+  if (n == 0) return PF_OK;
+  if (n > INT32_MAX / d->hq) return fail(PF_ERR_UNSUPPORTED, "n_tokens * n_heads above 2^31");
+  if (n > kMaxTokens) return fail(PF_ERR_UNSUPPORTED, "n_tokens above %lld", (long long)kMaxTokens);
+  if (packed_groups(*d, n, batch) > kMaxGroups || packed_key_groups(*d, n, batch) > kMaxGroups)
+    return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes: n_tokens * n_heads / 128 + batch * n_kv_heads must stay below 2^24");
+  if ((st = check_rows("q", q, n, d->hq, *d, false)) != PF_OK) return st;
+  if ((st = check_rows("k", k, n, d->hk, *d, false)) != PF_OK) return st;
+  if ((st = check_rows("v", v, n, d->hk, *d, false)) != PF_OK) return st;
+  if (!out || !lse) return fail(PF_ERR_INVALID_ARG, "out and lse must be non-NULL");
+  if (!aligned16(out) || !aligned4(lse)) return fail(PF_ERR_INVALID_ARG, "out must be 16-byte aligned, lse 4-byte");
+  return PF_OK;
+}
+
+static int check_tile_stride(const char* name, const pf_rows& r, int64_t n, const HeadsDims& d) {
+  if (n > 1 && r.token_stride * d.esize > ((int64_t)1 << 24))
+    return fail(PF_ERR_UNSUPPORTED, "%s: tokens more than 2^24 bytes apart", name);
+  return PF_OK;
+}
+
+int proxy_packed_attention_forward(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, const int32_t* cu_tokens,
+                                   const pf_rows* q, const pf_rows* k, const pf_rows* v, int64_t max_len,
+                                   int64_t window, int64_t sinks, float scale, void* out, float* lse, void* stream) {
+  HeadsDims d;
   const int64_t n = n_tokens;
-  const PagedPlan pl = paged_plan(d, c.batch, n, cu_tokens != nullptr, max_new, max_kv_len, window, sinks);
-  if (pl.groups > kMaxGroups / pl.slices)
-    return fail(PF_ERR_UNSUPPORTED, "more workgroups than one launch takes: n_tokens * n_heads / 16 + batch * n_kv_heads must stay below 2^24");
-  if ((st = check_rows("q", q, n, d.hq, d, false)) != PF_OK) return st;
-  if (!out) return fail(PF_ERR_INVALID_ARG, "out is NULL");
-  if (!aligned16(out)) return fail(PF_ERR_INVALID_ARG, "out must be 16-byte aligned");
-  if (!aligned4(lse)) return fail(PF_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-  if (pl.bytes && (!workspace || ws_bytes < pl.bytes))
-    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", pl.bytes, workspace ? ws_bytes : 0);
+  int st = check_packed(cfg, batch, n, cu_tokens, q, k, v, max_len, window, sinks, scale, out, lse, &d);
+  if (st != PF_OK || n == 0) return st;
+  if ((st = check_tile_stride("k", *k, n, d)) != PF_OK || (st = check_tile_stride("v", *v, n, d)) != PF_OK) return st;
+  const Extent wr[2] = {{out, (size_t)n * d.hq * d.d * d.esize}, {lse, (size_t)n * d.hq * sizeof(float)}};
+  const Extent rd[4] = {extent_of(q, n, d.hq, d), extent_of(k, n, d.hk, d), extent_of(v, n, d.hk, d),
+                        {cu_tokens, ((size_t)batch + 1) * sizeof(int32_t)}};
+  if (any_meet(wr, 2, rd, 4)) return fail(PF_ERR_INVALID_ARG, "out and lse must not overlap other buffers of the call");
+  const PackedCall c{n, max_len, cu_tokens, batch, rows_of(q), rows_of(k), rows_of(v), window, sinks, scale, out, lse};
+  return hip_status(launch_packed_forward(d, c, reinterpret_cast<hipStream_t>(stream)),
+                    "proxy_packed_attention_forward launch");
+}
+
+size_t proxy_packed_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens) {
+  HeadsDims d;
+  const char* why;
+  if (heads_dims(cfg, &d, &why) != PF_OK || batch < 1 || n_tokens < 1 || n_tokens > kMaxTokens) return 0;
+  return packed_backward_ws(d, n_tokens, batch);
+}
+
+int proxy_packed_attention_backward(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens,
+                                    const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k, const pf_rows* v,
+                                    int64_t max_len, int64_t window, int64_t sinks, float scale, const void* out,
+                                    const float* lse, const pf_rows* dout, const pf_rows* dq, const pf_rows* dk, const pf_rows* dv,
+                                    void* workspace, size_t ws_bytes, void* stream) {
+  HeadsDims d;
+  const int64_t n = n_tokens;
+  int st = check_packed(cfg, batch, n, cu_tokens, q, k, v, max_len, window, sinks, scale, out, lse, &d);
+  if (st != PF_OK || n == 0) return st;
+  if ((st = check_rows("dout", dout, n, d.hq, d, false)) != PF_OK) return st;
+  if ((st = check_rows("dq", dq, n, d.hq, d, true)) != PF_OK) return st;
+  if ((st = check_rows("dk", dk, n, d.hk, d, true)) != PF_OK) return st;
+  if ((st = check_rows("dv", dv, n, d.hk, d, true)) != PF_OK) return st;
+  if ((st = check_tile_stride("q", *q, n, d)) != PF_OK || (st = check_tile_stride("k", *k, n, d)) != PF_OK ||
+      (st = check_tile_stride("v", *v, n, d)) != PF_OK || (st = check_tile_stride("dout", *dout, n, d)) != PF_OK)
+    return st;
+  const size_t need = packed_backward_ws(d, n, batch);
+  if (!workspace || ws_bytes < need)
+    return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need, workspace ? ws_bytes : 0);
   if (!aligned16(workspace)) return fail(PF_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
-  const size_t pages = (size_t)c.n_pages * d.hk * c.page_size * d.d * d.esize;
-  const Extent wr[3] = {{out, (size_t)n * d.hq * d.d * d.esize},
-                        {lse, (size_t)n * d.hq * sizeof(float)},
-                        {workspace, pl.bytes}};
-  const Extent rd[6] = {extent_of(q, n, d.hq, d),
-                        {c.k, pages},
-                        {c.v, pages},
-                        {cache->page_table, (size_t)c.batch * cache->max_pages * sizeof(int32_t)},
-                        {cache->kv_len, (size_t)c.batch * sizeof(int32_t)},
-                        {cu_tokens, ((size_t)c.batch + 1) * sizeof(int32_t)}};
-  if (any_meet(wr, 3, rd, 6))
-    return fail(PF_ERR_INVALID_ARG, "out, lse and workspace must not overlap other buffers of the call");
-  return hip_status(launch_paged_attention(d, c, pl, n, cu_tokens, rows_of(q), scale, window, sinks, out, lse,
-                                           static_cast<char*>(workspace), reinterpret_cast<hipStream_t>(stream)),
-                    "proxy_paged_attention launch");
+  // dq, dk and dv may be bands of one buffer, as may q, k and v
+  if (rows_meet(*dq, d.hq, *dk, d.hk, n, d) || rows_meet(*dq, d.hq, *dv, d.hk, n, d) || rows_meet(*dk, d.hk, *dv, d.hk, n, d))
+    return fail(PF_ERR_INVALID_ARG, "dq, dk and dv must not overlap");
+  const pf_rows* in[4] = {q, k, v, dout};
+  const int ih[4] = {d.hq, d.hk, d.hk, d.hq};
+  for (int i = 0; i < 4; ++i)
+    if (rows_meet(*in[i], ih[i], *dq, d.hq, n, d) || rows_meet(*in[i], ih[i], *dk, d.hk, n, d) ||
+        rows_meet(*in[i], ih[i], *dv, d.hk, n, d))
+      return fail(PF_ERR_INVALID_ARG, "dq, dk and dv must not overlap what the call reads");
+  const Extent small[3] = {{out, (size_t)n * d.hq * d.d * d.esize},
+                           {lse, (size_t)n * d.hq * sizeof(float)},
+                           {cu_tokens, ((size_t)batch + 1) * sizeof(int32_t)}};
+  const Extent ws[1] = {{workspace, need}};
+  const Extent all[10] = {extent_of(q, n, d.hq, d),  extent_of(k, n, d.hk, d),  extent_of(v, n, d.hk, d),
+                          extent_of(dout, n, d.hq, d), extent_of(dq, n, d.hq, d), extent_of(dk, n, d.hk, d),
+                          extent_of(dv, n, d.hk, d), small[0],                  small[1],
+                          small[2]};
+  if (any_meet(ws, 1, all, 10)) return fail(PF_ERR_INVALID_ARG, "workspace must not overlap other buffers of the call");
+  for (int i = 4; i < 7; ++i)
+    if (any_meet(all + i, 1, small, 3))
+      return fail(PF_ERR_INVALID_ARG, "dq, dk and dv must not overlap what the call reads");
+  const PackedCall c{n, max_len, cu_tokens, batch, rows_of(q), rows_of(k), rows_of(v), window, sinks, scale,
+                     const_cast<void*>(out), const_cast<float*>(lse)};
+  const PackedOut o{rows_of(dout), rows_of(dq), rows_of(dk), rows_of(dv)};
+  return hip_status(launch_packed_backward(d, c, o, static_cast<char*>(workspace), reinterpret_cast<hipStream_t>(stream)),
+                    "proxy_packed_attention_backward launch");
 }
 
 }  // extern "C"

@@ -39,6 +39,8 @@ struct HeadsWeights {
 struct PagedDims {
   char* k;
   char* v;
+  uint8_t* k_scale;  // pages of 8 bits, else NULL
+  uint8_t* v_scale;
   int n_pages, page_size;
   const int32_t* table;
   int max_pages;
@@ -68,6 +70,23 @@ __device__ __forceinline__ int find_run(int count, F&& at, int64_t x) {
   return __builtin_amdgcn_readfirstlane(s);
 }
 
+// Where token `tok` of a call is in a cache: its row (head 0) in the pages, or -1
+// for one of no sequence or without a place; `at` is its row of the sequence,
+// kv_len - new + i for the i-th new token.
+__device__ __forceinline__ int64_t cache_place(const int32_t* cu, const int32_t* kv_len, const int32_t* table, int batch,
+                                               int max_pages, int n_pages, int hk, const FastDiv& fpage, int64_t tok,
+                                               int* at) {
+  const int s = cu ? find_run(batch + 1, [&](int c) { return cu[c]; }, tok) : (int)tok;
+  *at = 0;
+  if (s >= batch || (cu && tok < cu[s])) return -1;
+  const int64_t pos = cu ? (int64_t)kv_len[s] - cu[s + 1] + tok : (int64_t)kv_len[s] - 1;
+  if (pos < 0 || pos >= (int64_t)max_pages * fpage.d) return -1;
+  *at = (int)pos;
+  const int pg = fpage.div((int)pos);
+  const int id = table[(int64_t)s * max_pages + pg];
+  return id >= 0 && id < n_pages ? (int64_t)id * hk * fpage.d + ((int)pos - pg * fpage.d) : -1;
+}
+
 int heads_dims(const pf_heads_config* c, HeadsDims* d, const char** why);
 
 // Forward: q -> q_out, k -> k_out. n_tokens rows, positions [n_axes, n_tokens].
@@ -77,6 +96,10 @@ hipError_t launch_qk_forward(const HeadsDims& d, const HeadsWeights& w, int64_t 
 hipError_t launch_paged_append(const HeadsDims& d, const HeadsWeights& w, const PagedDims& c, int64_t n,
                                const int32_t* cu_tokens, const Rows& q, const Rows& k, const Rows& v,
                                const int32_t* positions, const Rows& q_out, hipStream_t s);
+// 8-bit pages back into rows of the config's type: those that an append of the
+// same tokens writes.
+hipError_t launch_paged_quant_read(const HeadsDims& d, const PagedDims& c, int64_t n, const int32_t* cu_tokens, const Rows& k_out,
+                              const Rows& v_out, hipStream_t s);
 size_t qk_backward_ws(const HeadsDims& d, int64_t n);
 hipError_t launch_qk_backward(const HeadsDims& d, const HeadsWeights& w, int64_t n, const Rows& q, const Rows& k,
                               const int32_t* positions, const Rows& dq_out, const Rows& dk_out, const Rows& dq,
@@ -93,9 +116,30 @@ struct PagedPlan {
   size_t bytes;
 };
 PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragged, int64_t max_new, int64_t max_kv_len,
-                     int64_t window, int64_t sinks);
+                     int64_t window, int64_t sinks, bool bits8);
 hipError_t launch_paged_attention(const HeadsDims& d, const PagedDims& c, const PagedPlan& pl, int64_t n_tokens,
                                   const int32_t* cu_tokens, const Rows& q, float scale, int64_t window, int64_t sinks,
                                   void* out, float* lse, char* ws, hipStream_t s);
+
+// Attention over whole sequences that lie one after another.
+struct PackedCall {
+  int64_t n_tokens, max_len;
+  const int32_t* cu;
+  int batch;
+  Rows q, k, v;
+  int64_t window, sinks;
+  float scale;
+  void* out;   // the backward reads out and lse
+  float* lse;
+};
+struct PackedOut {
+  Rows dout, dq, dk, dv;
+};
+// Workgroups by columns and by keys.
+int64_t packed_groups(const HeadsDims& d, int64_t n_tokens, int batch);
+int64_t packed_key_groups(const HeadsDims& d, int64_t n_tokens, int batch);
+size_t packed_backward_ws(const HeadsDims& d, int64_t n_tokens, int batch);
+hipError_t launch_packed_forward(const HeadsDims& d, const PackedCall& c, hipStream_t s);
+hipError_t launch_packed_backward(const HeadsDims& d, const PackedCall& c, const PackedOut& o, char* ws, hipStream_t s);
 
 }  // namespace pf

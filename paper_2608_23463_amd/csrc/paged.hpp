@@ -14,8 +14,11 @@ struct PagedParams {
   int64_t q_ts, q_hs;
   const char* k;
   const char* v;
+  const uint8_t* k_scale;  // pages of 8 bits: scale bytes of the rows
+  const uint8_t* v_scale;
+  int64_t k_ts, k_hs, v_ts, v_hs;  // packed rows, no pages: strides in elements
   const int32_t* table;
-  const int32_t* kv_len;
+  const int32_t* kv_len;  // NULL: packed rows, a sequence's tokens are its rows
   const int32_t* cu;    // NULL: one token of every sequence
   int n_pages, page_size, max_pages, batch, n_tokens;
   FastDiv page_blocks;  // blocks per page
@@ -53,6 +56,11 @@ struct Sequence {
       }
     }
     cols = n_new * p.group;
+    if (!p.kv_len) {
+      row0 = 0;
+      most = INT32_MAX;
+      return;
+    }
     const int64_t first = (int64_t)p.kv_len[s] - n_new;
     row0 = (int)(first < -n_new ? -n_new : first);
     most = p.max_pages * p.page_size;
@@ -101,8 +109,22 @@ struct Sight {
   }
 };
 
+// Where the rows of K and V are: pages in the rows' type, pages of 8 bits, or
+// packed rows in the order of the tokens.
+enum Source { kPages, kPages8, kPacked };
+
+// Factor of a scale byte, 2^(byte - 127) for bytes of 1 .. 254.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// Two neighbouring e4m3 values, the lower or the upper half of a word, times a
+// power of two: exact in bf16 and in fp32.
+template <bool UPPER>
+__device__ __forceinline__ uint32_t bf16_pair_of(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, UPPER));
+}
+
 // The prompts' kernel (bf16): out and lse, or with slices > 1 partial results
 // for the join.
-hipError_t launch_paged_prompt(const PagedParams& p, int d, int64_t groups, hipStream_t s);
+void launch_prompt(const PagedParams& p, int d, Source from, int64_t groups, hipStream_t s);
 
 }  // namespace pf

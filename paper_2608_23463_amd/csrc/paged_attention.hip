@@ -52,12 +52,13 @@ __device__ __forceinline__ float over_rows(float x, F&& f) {
   return f(__builtin_bit_cast(float, e), __builtin_bit_cast(float, o));
 }
 
-template <typename T, int D>
+template <typename T, int D, bool B8>
 struct Tile;
 
 // bf16: tiles of two blocks, one k step of the value product.
 template <int D>
-struct Tile<bf16, D> {
+struct Tile<bf16, D, false> {
+  typedef bf16 Stored;
   static constexpr int NB = 2, KS = D / 32, VE = D / 16, JJ = 1, NO = VE;
   static constexpr int kPerCu = D == 64 ? 4 : 3;  // workgroups that fit a CU's registers
   u32x4 k[NB][KS];
@@ -128,7 +129,8 @@ struct Tile<bf16, D> {
 // fp32: four rows per k step. Tiles of one block at D = 128 keep two tiles in
 // the registers.
 template <int D>
-struct Tile<float, D> {
+struct Tile<float, D, false> {
+  typedef float Stored;
   static constexpr int NB = D == 64 ? 2 : 1, KS = D / 16, VE = 4, JJ = D / 64, NO = 4 * JJ;
   static constexpr int kPerCu = 3;
   f32x4 k[NB][KS];
@@ -176,9 +178,162 @@ struct Tile<float, D> {
   }
 };
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, (Tile<T, D>::kPerCu)) paged_attention_kernel(PagedParams p) {
-  typedef Tile<T, D> Tl;
+// What rows of 8 bits share: a lane holds 16 channels of a row of K per load,
+// and of V the D / 16 neighbouring channels that it holds in bf16 too, so tiles
+// of four blocks are as many bytes as two in bf16. Values are widened where
+// they are used, times their row's power of two: exact in bf16 and fp32.
+template <int D>
+struct Raw8Tile {
+  typedef uint8_t Stored;
+  static constexpr int NB = 4, KL = D / 64, VE = D / 16, JJ = 1, NO = VE;
+  u32x4 k[NB][KL];
+  uint32_t v[NB][4][VE / 4];
+  uint32_t ks[NB], vs[NB];  // the scale byte of the lane's row of K, four of its rows of V
+  __device__ __forceinline__ void load_k(int b, const uint8_t* row, int g) {
+#pragma unroll
+    for (int s = 0; s < KL; ++s) k[b][s] = ld16(row + (4 * s + g) * 16);
+  }
+  __device__ __forceinline__ void load_v(int b, int r, const uint8_t* row, int m) {
+    if constexpr (VE == 8) {
+      const u32x2 t = *reinterpret_cast<const u32x2*>(row + VE * m);
+      v[b][r][0] = t[0];
+      v[b][r][1] = t[1];
+    } else {
+      v[b][r][0] = *reinterpret_cast<const uint32_t*>(row + VE * m);
+    }
+  }
+  __device__ __forceinline__ void zero_v(int b, int r) {
+#pragma unroll
+    for (int i = 0; i < VE / 4; ++i) v[b][r][i] = 0;
+    vs[b] = (vs[b] & ~(255u << (8 * r))) | 127u << (8 * r);
+  }
+  __device__ __forceinline__ float v_scale(int b, int r) const { return scale_of((vs[b] >> (8 * r)) & 255u); }
+};
+
+template <int D>
+struct Tile<bf16, D, true> : Raw8Tile<D> {
+  typedef Raw8Tile<D> R;
+  using R::k, R::v, R::ks, R::vs;
+  static constexpr int kPerCu = D == 64 ? 4 : 3;
+  struct Query {
+    bf16x8 f[2 * R::KL];
+    __device__ __forceinline__ void load(const bf16* row, int g, bool on) {
+#pragma unroll
+      for (int s = 0; s < 2 * R::KL; ++s) {
+        u32x4 t = {0u, 0u, 0u, 0u};
+        if (on) t = ld16(row + (4 * (s / 2) + g) * 16 + s % 2 * 8);
+        f[s] = __builtin_bit_cast(bf16x8, t);
+      }
+    }
+  };
+  __device__ __forceinline__ f32x4 scores(int b, const Query& q) const {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float f = scale_of(ks[b]);
+#pragma unroll
+    for (int i = 0; i < 2 * R::KL; ++i) {
+      u32x4 a;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t raw = k[b][i / 2][i % 2 * 2 + w];
+        a[2 * w] = bf16_pair_of<false>(raw, f);
+        a[2 * w + 1] = bf16_pair_of<true>(raw, f);
+      }
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), q.f[i], s, 0, 0, 0);
+    }
+    return s;
+  }
+  // (in two bf16 terms, as below the probabilities of a bf16 cache)
+  template <int E>  // channels E and E + 1 of the lane's
+  __device__ __forceinline__ void pair(int c, const bf16x8& hi, const bf16x8& lo, f32x4* o) const {
+    u32x4 a, z;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const uint32_t x = bf16_pair_of<(E & 2) != 0>(v[2 * c + b][r][E / 4], R::v_scale(2 * c + b, r));
+        const uint32_t y = bf16_pair_of<(E & 2) != 0>(v[2 * c + b][r + 1][E / 4], R::v_scale(2 * c + b, r + 1));
+        a[2 * b + r / 2] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+        z[2 * b + r / 2] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+      }
+    const bf16x8 f0 = __builtin_bit_cast(bf16x8, a), f1 = __builtin_bit_cast(bf16x8, z);
+    o[E] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0, hi, o[E], 0, 0, 0);
+    o[E + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1, hi, o[E + 1], 0, 0, 0);
+    o[E] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0, lo, o[E], 0, 0, 0);
+    o[E + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1, lo, o[E + 1], 0, 0, 0);
+  }
+  __device__ __forceinline__ void values(const float* p, f32x4* o) const {
+#pragma unroll
+    for (int c = 0; c < R::NB / 2; ++c) {
+      bf16x8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        hi[i] = (bf16)p[8 * c + i];
+        lo[i] = (bf16)(p[8 * c + i] - (float)hi[i]);
+      }
+      pair<0>(c, hi, lo, o);
+      pair<2>(c, hi, lo, o);
+      if constexpr (R::VE == 8) {
+        pair<4>(c, hi, lo, o);
+        pair<6>(c, hi, lo, o);
+      }
+    }
+  }
+};
+
+template <int D>
+struct Tile<float, D, true> : Raw8Tile<D> {
+  typedef Raw8Tile<D> R;
+  using R::k, R::v, R::ks, R::vs;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  static constexpr int kPerCu = 3;
+  struct Query {
+    f32x4 f[4 * R::KL];
+    __device__ __forceinline__ void load(const float* row, int g, bool on) {
+#pragma unroll
+      for (int s = 0; s < 4 * R::KL; ++s) {
+        f[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (on) f[s] = *reinterpret_cast<const f32x4*>(row + (4 * (s / 4) + g) * 16 + s % 4 * 4);
+      }
+    }
+  };
+  __device__ __forceinline__ f32x4 scores(int b, const Query& q) const {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float f = scale_of(ks[b]);
+#pragma unroll
+    for (int i = 0; i < 4 * R::KL; ++i) {
+      const uint32_t raw = k[b][i / 4][i % 4];
+      const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(raw, f, false);
+      const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(raw, f, true);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[0], q.f[i][0], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[1], q.f[i][1], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(y[0], q.f[i][2], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(y[1], q.f[i][3], s, 0, 0, 0);
+    }
+    return s;
+  }
+  __device__ __forceinline__ void values(const float* p, f32x4* o) const {
+#pragma unroll
+    for (int b = 0; b < R::NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float f = R::v_scale(b, r), w = p[4 * b + r];
+#pragma unroll
+        for (int i = 0; i < R::VE / 4; ++i) {
+          const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v[b][r][i], f, false);
+          const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v[b][r][i], f, true);
+          o[4 * i] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[0], w, o[4 * i], 0, 0, 0);
+          o[4 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[1], w, o[4 * i + 1], 0, 0, 0);
+          o[4 * i + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[0], w, o[4 * i + 2], 0, 0, 0);
+          o[4 * i + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[1], w, o[4 * i + 3], 0, 0, 0);
+        }
+      }
+  }
+};
+
+template <typename T, int D, bool B8>
+__global__ void __launch_bounds__(kThreads, (Tile<T, D, B8>::kPerCu)) paged_attention_kernel(PagedParams p) {
+  typedef Tile<T, D, B8> Tl;
+  typedef typename Tl::Stored Stored;
   constexpr int NB = Tl::NB, TR = NB * kBlock;
   __shared__ __attribute__((aligned(16))) float so[kWaves][kCols][D + 4];  // columns four banks apart
   __shared__ float sm[kWaves][kCols], sl[kWaves][kCols];
@@ -216,8 +371,8 @@ __global__ void __launch_bounds__(kThreads, (Tile<T, D>::kPerCu)) paged_attentio
 
   const int32_t* table = p.table + (int64_t)s * p.max_pages;
   const int64_t page_rows = (int64_t)p.hk * p.page_size;
-  const T* kp = reinterpret_cast<const T*>(p.k);
-  const T* vp = reinterpret_cast<const T*>(p.v);
+  const Stored* kp = reinterpret_cast<const Stored*>(p.k);
+  const Stored* vp = reinterpret_cast<const Stored*>(p.v);
 
   // A tile's blocks: their table entries as they are, and their first slots.
   struct Place {
@@ -242,18 +397,23 @@ __global__ void __launch_bounds__(kThreads, (Tile<T, D>::kPerCu)) paged_attentio
   // An entry that is no page reads page 0 instead, whose rows exist.
   auto is_page = [&](int id) { return (unsigned)id < (unsigned)p.n_pages; };
   auto base = [&](const Place& w, int b) {
-    return ((is_page(w.id[b]) ? w.id[b] : 0) * page_rows + (int64_t)hk * p.page_size + w.slot[b]) * D;
+    return (is_page(w.id[b]) ? w.id[b] : 0) * page_rows + (int64_t)hk * p.page_size + w.slot[b];
   };
   Tl t;
   auto fetch_k = [&](const Place& w) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) t.load_k(b, kp + base(w, b) + m * D, g);
+    for (int b = 0; b < NB; ++b) {
+      t.load_k(b, kp + base(w, b) * D + m * D, g);
+      if constexpr (B8) t.ks[b] = p.k_scale[base(w, b) + m];
+    }
   };
   auto fetch_v = [&](const Place& w) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) t.load_v(b, r, vp + base(w, b) + (4 * g + r) * D, m);
+      for (int r = 0; r < 4; ++r) t.load_v(b, r, vp + base(w, b) * D + (4 * g + r) * D, m);
+      if constexpr (B8) t.vs[b] = *reinterpret_cast<const uint32_t*>(p.v_scale + base(w, b) + 4 * g);
+    }
   };
 
   // The next tile's K is on its way from the moment the scores are formed and
@@ -426,17 +586,18 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(PagedParams p) {
 // token of 32 heads in 15 slices 13.2 us with a workgroup (14.5), in 64 21.8 (27.6).
 constexpr int kFewSlices = 8;
 
-template <typename T, int D>
+template <typename T, int D, Source FROM>
 hipError_t attention_on(const PagedParams& p, const PagedPlan& pl, hipStream_t s) {
   const bool tr = trace_on();
   hipError_t e;
-  if (tr) trace_begin(pl.prompt ? "paged_prompt" : "paged_attention", s);
-  if (pl.prompt) {
-    e = launch_paged_prompt(p, D, pl.groups, s);
-  } else {
-    paged_attention_kernel<T, D><<<dim3((unsigned)(pl.groups * pl.slices)), kThreads, 0, s>>>(p);
-    e = hipGetLastError();
-  }
+  if (tr)
+    trace_begin(FROM == kPages ? (pl.prompt ? "paged_prompt" : "paged_attention")
+                               : (pl.prompt ? "paged_quant_prompt" : "paged_quant_attention"), s);
+  if (pl.prompt)
+    launch_prompt(p, D, FROM, pl.groups, s);
+  else
+    paged_attention_kernel<T, D, FROM == kPages8><<<dim3((unsigned)(pl.groups * pl.slices)), kThreads, 0, s>>>(p);
+  e = hipGetLastError();
   if (tr) trace_end(s);
   if (e != hipSuccess || p.slices == 1) return e;
   if (tr) trace_begin("paged_join", s);
@@ -462,11 +623,11 @@ constexpr int64_t kPromptTokens = 32;
 }  // namespace
 
 PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragged, int64_t max_new, int64_t max_kv_len,
-                     int64_t window, int64_t sinks) {
+                     int64_t window, int64_t sinks, bool bits8) {
   PagedPlan pl;
   pl.prompt = d.esize == 2 && ragged && max_new >= kPromptTokens;
   pl.cols = pl.prompt ? 128 : kCols;
-  pl.tile_rows = pl.prompt ? 64 : kBlock * (d.esize == 4 && d.d == 128 ? 1 : 2);
+  pl.tile_rows = pl.prompt ? 64 : kBlock * (bits8 ? 4 : d.esize == 4 && d.d == 128 ? 1 : 2);
   window = std::min<int64_t>(window, INT32_MAX);
   sinks = std::min<int64_t>(sinks, INT32_MAX);
   max_new = std::min<int64_t>(max_new, n_tokens);
@@ -505,6 +666,8 @@ hipError_t launch_paged_attention(const HeadsDims& d, const PagedDims& c, const 
   p.q_hs = q.hs;
   p.k = c.k;
   p.v = c.v;
+  p.k_scale = c.k_scale;
+  p.v_scale = c.v_scale;
   p.table = c.table;
   p.kv_len = c.kv_len;
   p.cu = cu_tokens;
@@ -532,8 +695,12 @@ hipError_t launch_paged_attention(const HeadsDims& d, const PagedDims& c, const 
   p.lse = lse;
   p.part_o = reinterpret_cast<float*>(ws);
   p.part_ml = reinterpret_cast<float2*>(ws + (size_t)n_tokens * d.hq * pl.slices * d.d * sizeof(float));
-  if (d.esize == 2) return d.d == 64 ? attention_on<bf16, 64>(p, pl, s) : attention_on<bf16, 128>(p, pl, s);
-  return d.d == 64 ? attention_on<float, 64>(p, pl, s) : attention_on<float, 128>(p, pl, s);
+  if (c.k_scale) {
+    if (d.esize == 2) return d.d == 64 ? attention_on<bf16, 64, kPages8>(p, pl, s) : attention_on<bf16, 128, kPages8>(p, pl, s);
+    return d.d == 64 ? attention_on<float, 64, kPages8>(p, pl, s) : attention_on<float, 128, kPages8>(p, pl, s);
+  }
+  if (d.esize == 2) return d.d == 64 ? attention_on<bf16, 64, kPages>(p, pl, s) : attention_on<bf16, 128, kPages>(p, pl, s);
+  return d.d == 64 ? attention_on<float, 64, kPages>(p, pl, s) : attention_on<float, 128, kPages>(p, pl, s);
 }
 
 }  // namespace pf

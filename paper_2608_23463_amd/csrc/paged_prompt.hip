@@ -37,7 +37,7 @@ constexpr int kColumns = 128;
 // with two 56, four of 4,096 tokens behind 16,384 rows 1,347 and 1,516; one of
 // 8,192 tokens, a round and a half of workgroups, 195 and 173), two at 128, whose
 // accumulators take the registers of a third.
-template <int D>
+template <int D, Source FROM>
 __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel(PagedParams p) {
   constexpr int RB = D * 2, CH = RB / 16;     // bytes and 16-byte chunks of a row
   constexpr int kTileBytes = kTile * RB, kStage = 2 * kTileBytes;
@@ -95,6 +95,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
     }
   }
 
+  constexpr bool kPaged = FROM != kPacked;
   const int32_t* table = p.table + (int64_t)s * p.max_pages;
   const int page_rows = p.hk * p.page_size;  // a cache has fewer than 2^31 rows
   auto tile_row = [&](int t) { return sight.tile(first + t) * kTile; };
@@ -111,12 +112,85 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
     const bool have = blk16 * kBlock <= sight.last && (unsigned)id < (unsigned)p.n_pages;
     return have ? id * page_rows + hk * p.page_size + (blk16 - pg * p.page_blocks.d) * kBlock : -1;
   };
+  // value rows that no column sees land as zeros: whether a tile has none
+  auto all_seen = [&](int r0) {
+    return r0 + kTile - 1 <= sight.first && (r0 > sight.top - p.window || r0 + kTile <= p.sinks);
+  };
+  auto unseen = [&](int j) { return j > sight.last || (j <= sight.first - p.window && j >= p.sinks); };
+  // Packed rows: starts the loads of a tile. Rows past the last that is seen
+  // may be another sequence's or past the tensor's end.
+  auto issue_packed = [&](int t, int stage) {
+    const int r0 = tile_row(t), j0 = r0 + wave * kBlock;
+    const bool all = all_seen(r0);
+    const rsrc_t rk = make_rsrc_uniform(p.k + ((int64_t)(sq.t0 + j0) * p.k_ts + hk * p.k_hs) * 2, kOOB - 1);
+    const rsrc_t rv = make_rsrc_uniform(p.v + ((int64_t)(sq.t0 + j0) * p.v_ts + hk * p.v_hs) * 2, kOOB - 1);
+    char* st = smem + stage * kStage + wave * kBlock * RB;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = j * kRowsPerLoad + lane / CH, c = lane % CH;
+      uint32_t off = (uint32_t)(r * (int)p.k_ts * 2 + lds_swz<CH>(wave * kBlock + r, c) * 16);
+      if (!all && j0 + r > sight.last) off = kOOB;
+      buf_ld16_lds(rk, off, st + j * 1024);
+    }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = j * kRowsPerLoad + lane / CH, c = lane % CH;
+      uint32_t off = (uint32_t)(r * (int)p.v_ts * 2 + vtr_swz<CH>(wave * kBlock + r, c) * 16);
+      if (!all && unseen(j0 + r)) off = kOOB;
+      buf_ld16_lds(rv, off, st + kTileBytes + j * 1024);
+    }
+  };
+  // Pages of 8 bits: a tile's rows come into registers, 16 values per lane and
+  // load, and are widened on their way to LDS, where the values are those of a
+  // bf16 cache (a power of two times e4m3 is exact in bf16).
+  constexpr int C8 = D / 16, kLoads8 = kBlock * C8 / kWave, kRows8 = kWave / C8;
+  u32x4 raw_k[kLoads8], raw_v[kLoads8];
+  uint32_t byte_k[kLoads8], byte_v[kLoads8];
+  auto fetch8 = [&](int t, int rows, int at) {
+    const int r0 = tile_row(t);
+    const int mine16 = __builtin_amdgcn_readlane(rows, at + wave);
+    const bool all = all_seen(r0);
+    const int64_t row = mine16 < 0 ? 0 : mine16;
+    const uint32_t n = mine16 < 0 ? 0 : kBlock;
+    const rsrc_t rk = make_rsrc_uniform(p.k + row * D, n * D), rv = make_rsrc_uniform(p.v + row * D, n * D);
+    const rsrc_t sk = make_rsrc_uniform(p.k_scale + row, n), sv = make_rsrc_uniform(p.v_scale + row, n);
+#pragma unroll
+    for (int j = 0; j < kLoads8; ++j) {
+      const int r = j * kRows8 + lane / C8, c = lane % C8;
+      const bool none = !all && unseen(r0 + wave * kBlock + r);
+      raw_k[j] = buf_ld16(rk, (uint32_t)(r * D + c * 16));
+      raw_v[j] = buf_ld16(rv, none ? kOOB : (uint32_t)(r * D + c * 16));
+      byte_k[j] = __builtin_amdgcn_raw_buffer_load_b8(sk, r, 0, 0);
+      byte_v[j] = __builtin_amdgcn_raw_buffer_load_b8(sv, none ? kOOB : (uint32_t)r, 0, 0);
+    }
+  };
+  auto put8 = [&](int stage) {
+    char* st = smem + stage * kStage;
+#pragma unroll
+    for (int j = 0; j < kLoads8; ++j) {
+      const int r = wave * kBlock + j * kRows8 + lane / C8, c = lane % C8;
+      const float fk = scale_of(byte_k[j]), fv = scale_of(byte_v[j]);
+      u32x4 k[2], v[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        k[i / 2][i % 2 * 2] = bf16_pair_of<false>(raw_k[j][i], fk);
+        k[i / 2][i % 2 * 2 + 1] = bf16_pair_of<true>(raw_k[j][i], fk);
+        v[i / 2][i % 2 * 2] = bf16_pair_of<false>(raw_v[j][i], fv);
+        v[i / 2][i % 2 * 2 + 1] = bf16_pair_of<true>(raw_v[j][i], fv);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        *reinterpret_cast<u32x4*>(st + r * RB + lds_swz<CH>(r, 2 * c + h) * 16) = k[h];
+        *reinterpret_cast<u32x4*>(st + kTileBytes + r * RB + vtr_swz<CH>(r, 2 * c + h) * 16) = v[h];
+      }
+    }
+  };
   // Starts the loads of a tile whose blocks are `rows`' from lane `at` on.
   auto issue = [&](int t, int stage, int rows, int at) {
     const int r0 = tile_row(t);
     const int mine16 = __builtin_amdgcn_readlane(rows, at + wave);
-    // a block without a page, and value rows that no column sees, land as zeros
-    const bool all = r0 + kTile - 1 <= sight.first && (r0 > sight.top - p.window || r0 + kTile <= p.sinks);
+    // a block without a page lands as zeros too
+    const bool all = all_seen(r0);
     const uint32_t bytes = mine16 < 0 ? 0 : kBlock * RB;
     const int64_t base = mine16 < 0 ? 0 : (int64_t)mine16 * RB;
     const rsrc_t rk = make_rsrc_uniform(p.k + base, bytes), rv = make_rsrc_uniform(p.v + base, bytes);
@@ -130,10 +204,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
     for (int j = 0; j < kLoads; ++j) {
       const int r = j * kRowsPerLoad + lane / CH, c = lane % CH;
       uint32_t off = (uint32_t)(r * RB + vtr_swz<CH>(wave * kBlock + r, c) * 16);
-      if (!all) {
-        const int jr = r0 + wave * kBlock + r;
-        if (jr > sight.last || (jr <= sight.first - p.window && jr >= p.sinks)) off = kOOB;
-      }
+      if (!all && unseen(r0 + wave * kBlock + r)) off = kOOB;
       buf_ld16_lds(rv, off, st + kTileBytes + j * 1024);
     }
   };
@@ -154,20 +225,36 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
 
   int rows = -1, rows_next = -1;  // of 16 tiles, and of the 16 behind them
   if (ntiles > 0) {
-    rows = blocks_of(0);
-    rows_next = blocks_of(kAhead);
-    issue(0, 0, rows, 0);
+    if constexpr (kPaged) {
+      rows = blocks_of(0);
+      rows_next = blocks_of(kAhead);
+    }
+    if constexpr (FROM == kPages) issue(0, 0, rows, 0);
+    if constexpr (FROM == kPacked) issue_packed(0, 0);
+    if constexpr (FROM == kPages8) {
+      fetch8(0, rows, 0);
+      put8(0);
+      if (ntiles > 1) fetch8(1, rows, kPerTile);
+    }
   }
   for (int t = 0; t < ntiles; ++t) {
     const int r0 = tile_row(t), in = t % kAhead;
-    wait_vmcnt<0>();
+    if constexpr (FROM != kPages8) wait_vmcnt<0>();
     lds_barrier();  // tile t landed for all; every wave is done with tile t - 1
-    const int gone = (int)(__builtin_amdgcn_ballot_w64(rows < 0) >> (in * kPerTile)) & ((1 << kPerTile) - 1);
-    if (in == kAhead - 1) {
+    const int gone =
+        kPaged ? (int)(__builtin_amdgcn_ballot_w64(rows < 0) >> (in * kPerTile)) & ((1 << kPerTile) - 1) : 0;
+    if (kPaged && in == kAhead - 1) {
       rows = rows_next;
       if (t + 1 + kAhead < ntiles) rows_next = blocks_of(t + 1 + kAhead);
     }
-    if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1, rows, (t + 1) % kAhead * kPerTile);
+    if constexpr (FROM == kPages) {
+      if (t + 1 < ntiles) issue(t + 1, (t + 1) & 1, rows, (t + 1) % kAhead * kPerTile);
+    } else if constexpr (FROM == kPacked) {
+      if (t + 1 < ntiles) issue_packed(t + 1, (t + 1) & 1);
+    } else {  // the next tile's registers to LDS, and the one behind it into them
+      if (t + 1 < ntiles) put8((t + 1) & 1);
+      if (t + 2 < ntiles) fetch8(t + 2, in == kAhead - 2 ? rows_next : rows, (t + 2) % kAhead * kPerTile);
+    }
     const char* sk = smem + (t & 1) * kStage;
     const char* sv = sk + kTileBytes;
     if (r0 > wlast || (r0 + kTile - 1 <= wlow && r0 >= p.sinks)) continue;  // wave-uniform: nothing it sees
@@ -336,13 +423,17 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
 
 }  // namespace
 
-hipError_t launch_paged_prompt(const PagedParams& p, int d, int64_t groups, hipStream_t s) {
+void launch_prompt(const PagedParams& p, int d, Source from, int64_t groups, hipStream_t s) {
   const dim3 grid((unsigned)(groups * p.slices));
-  if (d == 64)
-    paged_prompt_kernel<64><<<grid, kThreads, 0, s>>>(p);
+  if (from == kPacked)
+    d == 64 ? paged_prompt_kernel<64, kPacked><<<grid, kThreads, 0, s>>>(p)
+            : paged_prompt_kernel<128, kPacked><<<grid, kThreads, 0, s>>>(p);
+  else if (from == kPages8)
+    d == 64 ? paged_prompt_kernel<64, kPages8><<<grid, kThreads, 0, s>>>(p)
+            : paged_prompt_kernel<128, kPages8><<<grid, kThreads, 0, s>>>(p);
   else
-    paged_prompt_kernel<128><<<grid, kThreads, 0, s>>>(p);
-  return hipGetLastError();
+    d == 64 ? paged_prompt_kernel<64, kPages><<<grid, kThreads, 0, s>>>(p)
+            : paged_prompt_kernel<128, kPages><<<grid, kThreads, 0, s>>>(p);
 }
 
 }  // namespace pf

@@ -112,6 +112,8 @@ struct QkParams {
   // append
   char* k_pages;
   char* v_pages;
+  uint8_t* k_scale;  // pages of 8 bits
+  uint8_t* v_scale;
   const int32_t* table;
   const int32_t* kv_len;
   const int32_t* cu;
@@ -195,6 +197,21 @@ __device__ __forceinline__ float row_sum(float v) {
   return v;
 }
 
+// Largest over those lanes, of values that are not negative (a lane outside the
+// row would give zero).
+template <int CTRL>
+__device__ __forceinline__ float max_lane(float v) {
+  return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)));
+}
+template <int LPR>
+__device__ __forceinline__ float row_max(float v) {
+  static_assert(LPR == 4 || LPR == 8, "lanes of a row");
+  v = max_lane<0xb1>(v);
+  v = max_lane<0x4e>(v);
+  if (LPR == 8) v = max_lane<0x141>(v);
+  return v;
+}
+
 template <typename T>
 __device__ __forceinline__ void load16(const T* p, int a, int b, Raw8<T>* r) {
   raw_load8(p + a, r[0]);
@@ -248,30 +265,67 @@ __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, floa
 }
 
 // Where a token of an append goes: its row (head 0) in the pages, or -1 for one
-// of no sequence or without a place; `at` is its row of the sequence, kv_len -
-// new + i for the i-th new token.
+// of no sequence or without a place; `at` is its row of the sequence.
 __device__ __forceinline__ int64_t place_of(const QkParams& p, int64_t tok, int* at) {
-  const int s = p.cu ? find_run(p.batch + 1, [&](int c) { return p.cu[c]; }, tok) : (int)tok;
-  *at = 0;
-  if (s >= p.batch || (p.cu && tok < p.cu[s])) return -1;
-  const int64_t pos = p.cu ? (int64_t)p.kv_len[s] - p.cu[s + 1] + tok : (int64_t)p.kv_len[s] - 1;
-  if (pos < 0 || pos >= (int64_t)p.max_pages * p.page_size) return -1;
-  *at = (int)pos;
-  const int pg = p.fpage.div((int)pos);
-  const int id = p.table[(int64_t)s * p.max_pages + pg];
-  return id >= 0 && id < p.n_pages ? (int64_t)id * p.hk * p.page_size + ((int)pos - pg * p.page_size) : -1;
+  return cache_place(p.cu, p.kv_len, p.table, p.batch, p.max_pages, p.n_pages, p.hk, p.fpage, tok, at);
 }
 
-// Destination of a row of token `tok`, whose place is `place` in an append.
-template <typename T, int D, bool APPEND>
-__device__ __forceinline__ T* destination(const QkParams& p, const Tensor& x, int64_t tok, int h, int64_t place) {
-  if (!APPEND || x.which == 0) return reinterpret_cast<T*>(x.out.p) + tok * x.out.ts + h * x.out.hs;
-  return reinterpret_cast<T*>(x.which == 1 ? p.k_pages : p.v_pages) + (place + (int64_t)h * p.page_size) * D;
+// What a launch does with the rows: turned ones to tensors, or keys and values
+// into pages of the rows' type or of 8 bits.
+enum Mode { kTurn, kAppend, kAppend8 };
+
+// The lane's 16 elements of a row, turned, to their place: tensors, or pages
+// where `place` is the token's row.
+//
+// In 8 bits a row is codes in e4m3, to nearest even, of x 2^-e with the smallest
+// e that takes the row's largest finite magnitude to at most 448 (and at least
+// -110), and e + 127 as a byte: the multiplication is exact, so each element is
+// rounded once. A floating code needs no finer scale than a power of two: its
+// steps go by the value. What is not finite is held as NaN.
+template <typename T, int D, Mode MODE>
+__device__ __forceinline__ void put_row(const QkParams& p, const Tensor& x, int64_t tok, int h, bool on, int64_t place,
+                                        int a, int b, float* v) {
+  if (MODE != kAppend8 || x.which == 0) {
+    if (!on) return;
+    T* dst = MODE == kTurn || x.which == 0
+                 ? reinterpret_cast<T*>(x.out.p) + tok * x.out.ts + h * x.out.hs
+                 : reinterpret_cast<T*>(x.which == 1 ? p.k_pages : p.v_pages) + (place + (int64_t)h * p.page_size) * D;
+    store8(dst + a, v);
+    store8(dst + b, v + 8);
+    return;
+  }
+  float top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float m = fabsf(v[i]);
+    top = fmaxf(top, m < INFINITY ? m : 0.0f);
+  }
+  top = row_max<D / 16>(top);
+  const uint32_t bits = __builtin_bit_cast(uint32_t, top);
+  const int byte = max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 17);
+  const float inv = __builtin_bit_cast(float, (uint32_t)(254 - byte) << 23);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = fabsf(v[4 * i + e]) < INFINITY ? v[4 * i + e] * inv : NAN;
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+    w[i] = (uint32_t)c;
+  }
+  if (!on) return;
+  const int64_t row = place + (int64_t)h * p.page_size;
+  char* dst = (x.which == 1 ? p.k_pages : p.v_pages) + row * D;
+  *reinterpret_cast<uint2*>(dst + a) = make_uint2(w[0], w[1]);
+  *reinterpret_cast<uint2*>(dst + b) = make_uint2(w[2], w[3]);
+  if (threadIdx.x % (D / 16) == 0) (x.which == 1 ? p.k_scale : p.v_scale)[row] = (uint8_t)byte;
 }
 
 // Many tokens: TPW of them per wave, all their rows.
-template <typename T, int D, bool PAIRS, int TPW, bool APPEND>
+template <typename T, int D, bool PAIRS, int TPW, Mode MODE>
 __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p) {
+  constexpr bool APPEND = MODE != kTurn;
   constexpr int LPR = D / 16, RPP = kWave / LPR;  // lanes per row, rows per pass
   __shared__ float2 turns[kWaves][TPW][D / 2];
   __shared__ int64_t places[kWaves][TPW];
@@ -315,19 +369,16 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p) {
       raw_to_f32(r[1], v + 8);
       norm_and_turn<D, PAIRS>(p, which, v, g, &turns[wave][tk][8 * (lane % LPR)], ch.turned);
       const int64_t place = APPEND ? places[wave][tk] : 0;
-      if (on && place >= 0) {
-        T* dst = destination<T, D, APPEND>(p, x, t0 + tk, h, place);
-        store8(dst + ch.a, v);
-        store8(dst + ch.b, v + 8);
-      }
+      put_row<T, D, MODE>(p, x, t0 + tk, h, on && place >= 0, place, ch.a, ch.b, v);
     }
   }
 }
 
 // Few tokens: a wave for every RPP rows of every token, whose loads are on
 // their way while it finds the token's place and its turns.
-template <typename T, int D, bool PAIRS, bool APPEND>
+template <typename T, int D, bool PAIRS, Mode MODE>
 __global__ void __launch_bounds__(kThreads) qk_few_kernel(QkParams p) {
+  constexpr bool APPEND = MODE != kTurn;
   constexpr int LPR = D / 16, RPP = kWave / LPR;
   __shared__ float2 turns[kWaves][D / 2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -362,11 +413,7 @@ __global__ void __launch_bounds__(kThreads) qk_few_kernel(QkParams p) {
   raw_to_f32(r[0], v);
   raw_to_f32(r[1], v + 8);
   norm_and_turn<D, PAIRS>(p, which, v, g, &turns[wave][8 * (lane % LPR)], ch.turned);
-  if (on && place >= 0) {
-    T* dst = destination<T, D, APPEND>(p, x, tok, h, place);
-    store8(dst + ch.a, v);
-    store8(dst + ch.b, v + 8);
-  }
+  put_row<T, D, MODE>(p, x, tok, h, on && place >= 0, place, ch.a, ch.b, v);
 }
 
 struct QkBwdParams {
@@ -537,30 +584,21 @@ TurnParams turn_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, con
   return t;
 }
 
-template <class F>
-hipError_t timed(const char* label, hipStream_t s, F&& f) {
-  const bool tr = trace_on();
-  if (tr) trace_begin(label, s);
-  f();
-  const hipError_t e = hipGetLastError();
-  if (tr) trace_end(s);
-  return e;
-}
-
 // Tokens below which a wave takes one pass: 2,000 x (16 + 16) x 64 6.5 us (7.0
 // with a wave per token), an append of 500 x (16 + 16 + 16) x 64 5.8 (7.6), of
 // 4,000 x (32 + 8 + 8) x 128 22.7 (20.8).
 constexpr int64_t kFewTokens = 2048;
 
-template <typename T, int D, bool PAIRS, bool APPEND>
+template <typename T, int D, bool PAIRS, Mode MODE>
 hipError_t forward_on(QkParams p, int64_t n, const char* label, hipStream_t s) {
+  constexpr bool APPEND = MODE != kTurn;
   constexpr int RPP = kWave / (D / 16);
   return timed(label, s, [&] {
     if (n < kFewTokens) {
       const int pk = (p.hk + RPP - 1) / RPP;
       p.fparts = FastDiv((p.q.p ? (p.hq + RPP - 1) / RPP : 0) + (APPEND ? 2 * pk : pk));
       const int64_t units = n * p.fparts.d;
-      qk_few_kernel<T, D, PAIRS, APPEND><<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
+      qk_few_kernel<T, D, PAIRS, MODE><<<dim3((unsigned)((units + kWaves - 1) / kWaves)), kThreads, 0, s>>>(p);
     } else {
       // One token per wave while its rows fill the passes to two thirds: its
       // loads start earliest (65,536 x (16 + 4) x 128: 127 us, with four tokens
@@ -572,23 +610,23 @@ hipError_t forward_on(QkParams p, int64_t n, const char* label, hipStream_t s) {
       const int per = kWaves * (single ? 1 : 4);
       const dim3 grid((unsigned)((n + per - 1) / per));
       if (single)
-        qk_forward_kernel<T, D, PAIRS, 1, APPEND><<<grid, kThreads, 0, s>>>(p);
+        qk_forward_kernel<T, D, PAIRS, 1, MODE><<<grid, kThreads, 0, s>>>(p);
       else
-        qk_forward_kernel<T, D, PAIRS, 4, APPEND><<<grid, kThreads, 0, s>>>(p);
+        qk_forward_kernel<T, D, PAIRS, 4, MODE><<<grid, kThreads, 0, s>>>(p);
     }
   });
 }
 
-template <bool APPEND>
+template <Mode MODE>
 hipError_t forward_any(const HeadsDims& d, const QkParams& p, int64_t n, const char* label, hipStream_t s) {
   if (d.esize == 2) {
     if (d.d == 64)
-      return d.pairs_style ? forward_on<bf16, 64, true, APPEND>(p, n, label, s) : forward_on<bf16, 64, false, APPEND>(p, n, label, s);
-    return d.pairs_style ? forward_on<bf16, 128, true, APPEND>(p, n, label, s) : forward_on<bf16, 128, false, APPEND>(p, n, label, s);
+      return d.pairs_style ? forward_on<bf16, 64, true, MODE>(p, n, label, s) : forward_on<bf16, 64, false, MODE>(p, n, label, s);
+    return d.pairs_style ? forward_on<bf16, 128, true, MODE>(p, n, label, s) : forward_on<bf16, 128, false, MODE>(p, n, label, s);
   }
   if (d.d == 64)
-    return d.pairs_style ? forward_on<float, 64, true, APPEND>(p, n, label, s) : forward_on<float, 64, false, APPEND>(p, n, label, s);
-  return d.pairs_style ? forward_on<float, 128, true, APPEND>(p, n, label, s) : forward_on<float, 128, false, APPEND>(p, n, label, s);
+    return d.pairs_style ? forward_on<float, 64, true, MODE>(p, n, label, s) : forward_on<float, 64, false, MODE>(p, n, label, s);
+  return d.pairs_style ? forward_on<float, 128, true, MODE>(p, n, label, s) : forward_on<float, 128, false, MODE>(p, n, label, s);
 }
 
 QkParams qk_params(const HeadsDims& d, const HeadsWeights& w, int64_t n, const int32_t* positions) {
@@ -636,7 +674,7 @@ hipError_t launch_qk_forward(const HeadsDims& d, const HeadsWeights& w, int64_t 
   p.k = k;
   p.q_out = q_out;
   p.k_out = k_out;
-  return forward_any<false>(d, p, n, "qk_norm_rope", s);
+  return forward_any<kTurn>(d, p, n, "qk_norm_rope", s);
 }
 
 hipError_t launch_paged_append(const HeadsDims& d, const HeadsWeights& w, const PagedDims& c, int64_t n,
@@ -657,7 +695,9 @@ hipError_t launch_paged_append(const HeadsDims& d, const HeadsWeights& w, const 
   p.max_pages = c.max_pages;
   p.batch = c.batch;
   p.fpage = FastDiv(c.page_size);
-  return forward_any<true>(d, p, n, "paged_append", s);
+  p.k_scale = c.k_scale;
+  p.v_scale = c.v_scale;
+  return c.k_scale ? forward_any<kAppend8>(d, p, n, "paged_quant_append", s) : forward_any<kAppend>(d, p, n, "paged_append", s);
 }
 
 size_t qk_backward_ws(const HeadsDims& d, int64_t n) {

@@ -11,4 +11,15 @@ bool trace_on();
 void trace_begin(const char* label, hipStream_t stream);
 void trace_end(hipStream_t stream);
 
+// f's launches under a label; the last launch error.
+template <class F>
+hipError_t timed(const char* label, hipStream_t s, F&& f) {
+  const bool tr = trace_on();
+  if (tr) trace_begin(label, s);
+  f();
+  const hipError_t e = hipGetLastError();
+  if (tr) trace_end(s);
+  return e;
+}
+
 }  // namespace pf
