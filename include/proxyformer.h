@@ -569,7 +569,8 @@ int proxy_packed_attention_forward(const pf_heads_config* cfg, int32_t batch, in
  * may be bands of one buffer. workspace: proxy_packed_workspace_size bytes
  * (0 for invalid sizes), 16-byte aligned, overlapping nothing else; calls that
  * may run at the same time need workspaces of their own. */
-size_t proxy_packed_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens);
+size_t proxy_packed_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int64_t max_len,
+                                   int64_t window, int64_t sinks);
 int proxy_packed_attention_backward(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens,
                                     const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k, const pf_rows* v,
                                     int64_t max_len, int64_t window, int64_t sinks, float scale, const void* out,

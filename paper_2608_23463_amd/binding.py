@@ -260,7 +260,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.proxy_packed_attention_forward.argtypes = [P(PfHeadsConfig), c_int32, c_int64, c_void_p, rows, rows, rows, c_int64,
                                                    c_int64, c_int64, ctypes.c_float, c_void_p, c_void_p, c_void_p]
     lib.proxy_packed_attention_forward.restype = c_int32
-    lib.proxy_packed_workspace_size.argtypes = [P(PfHeadsConfig), c_int32, c_int64]
+    lib.proxy_packed_workspace_size.argtypes = [P(PfHeadsConfig), c_int32, c_int64, c_int64, c_int64, c_int64]
     lib.proxy_packed_workspace_size.restype = c_size_t
     lib.proxy_packed_attention_backward.argtypes = [P(PfHeadsConfig), c_int32, c_int64, c_void_p, rows, rows, rows, c_int64,
                                                     c_int64, c_int64, ctypes.c_float, c_void_p, c_void_p, rows, rows, rows,
@@ -825,7 +825,7 @@ def packed_attention_backward(cfg: PfHeadsConfig, q, k, v, out, lse, dout, cu_to
         dv = _empty((n, hk, cfg.head_dim), q.dtype, dev)
     wq, wk, wv = _rows(cfg, "dq", dq, n, hq, dev), _rows(cfg, "dk", dk, n, hk, dev), _rows(cfg, "dv", dv, n, hk, dev)
     if workspace is None:
-        workspace = _bytes(int(lib.proxy_packed_workspace_size(cfg, batch, n)), dev)
+        workspace = _bytes(int(lib.proxy_packed_workspace_size(cfg, batch, n, max_len, window, sinks)), dev)
     ws, ws_bytes = _workspace(workspace, dev)
     _check(lib.proxy_packed_attention_backward(cfg, batch, n, cu, rq, rk, rv, max_len, window, sinks,
                                                cfg.head_dim ** -0.5 if scale is None else scale, to, tl, ro, wq, wk, wv, ws,

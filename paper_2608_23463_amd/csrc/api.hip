@@ -949,11 +949,14 @@ int proxy_packed_attention_forward(const pf_heads_config* cfg, int32_t batch, in
                     "proxy_packed_attention_forward launch");
 }
 
-size_t proxy_packed_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens) {
+size_t proxy_packed_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int64_t max_len,
+                                   int64_t window, int64_t sinks) {
   HeadsDims d;
   const char* why;
-  if (heads_dims(cfg, &d, &why) != PF_OK || batch < 1 || n_tokens < 1 || n_tokens > kMaxTokens) return 0;
-  return packed_backward_ws(d, n_tokens, batch);
+  if (heads_dims(cfg, &d, &why) != PF_OK || batch < 1 || n_tokens < 1 || n_tokens > kMaxTokens || max_len < 1 ||
+      window < 0 || sinks < 0)
+    return 0;
+  return packed_backward_ws(d, n_tokens, batch, max_len, window, sinks);
 }
 
 int proxy_packed_attention_backward(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens,
@@ -972,7 +975,7 @@ int proxy_packed_attention_backward(const pf_heads_config* cfg, int32_t batch, i
   if ((st = check_tile_stride("q", *q, n, d)) != PF_OK || (st = check_tile_stride("k", *k, n, d)) != PF_OK ||
       (st = check_tile_stride("v", *v, n, d)) != PF_OK || (st = check_tile_stride("dout", *dout, n, d)) != PF_OK)
     return st;
-  const size_t need = packed_backward_ws(d, n, batch);
+  const size_t need = packed_backward_ws(d, n, batch, max_len, window, sinks);
   if (!workspace || ws_bytes < need)
     return fail(PF_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need, workspace ? ws_bytes : 0);
   if (!aligned16(workspace)) return fail(PF_ERR_INVALID_ARG, "workspace must be 16-byte aligned");

@@ -138,7 +138,7 @@ struct PackedOut {
 // Workgroups by columns and by keys.
 int64_t packed_groups(const HeadsDims& d, int64_t n_tokens, int batch);
 int64_t packed_key_groups(const HeadsDims& d, int64_t n_tokens, int batch);
-size_t packed_backward_ws(const HeadsDims& d, int64_t n_tokens, int batch);
+size_t packed_backward_ws(const HeadsDims& d, int64_t n_tokens, int batch, int64_t max_len, int64_t window, int64_t sinks);
 hipError_t launch_packed_forward(const HeadsDims& d, const PackedCall& c, hipStream_t s);
 hipError_t launch_packed_backward(const HeadsDims& d, const PackedCall& c, const PackedOut& o, char* ws, hipStream_t s);
 

@@ -23,7 +23,11 @@ struct PackedGrads {
   int64_t stat_rows;
   float scale;
   int key_blocks;     // of a K/V head
-  FastDiv fkey_blocks;
+  // the queries of a block of keys are cut into at most `slices` runs of at
+  // least min_tiles tiles, whose sums are joined
+  int slices;
+  FastDiv fslices, fmin_tiles;
+  float* part;
 };
 
 // A sequence's statistics begin at a multiple of four, so tiles of them load in
@@ -43,14 +47,19 @@ struct BothWays {
     if constexpr (CH == 16) return c ^ ((r & 3) << 2 | ((r >> 2) & 3));
     return c ^ (((r >> 1) & 1) << 2 | ((r >> 2) & 3));
   }
-  // row r, channels 16 kk + 8 g ..
-  static __device__ __forceinline__ frag row(const char* t, int r, int kk, int g) {
-    const char* p = t + r * RB;
+  // Reads go by a lane's base offset, formed once: the swizzles of the steps are
+  // exclusive ors with constants, as a row's bytes are a power of two.
+  // Rows: lane % 32 of the tile, channels 16 kk + 8 (lane / 32) ..
+  static __device__ __forceinline__ uint32_t row_base(int lane) {
+    const int r = lane & 31, g = lane >> 5;
+    return (uint32_t)(r * RB + swz(r, sizeof(T) == 2 ? g : 2 * g) * 16);
+  }
+  static __device__ __forceinline__ frag row(const char* t, uint32_t base, int kk) {
     if constexpr (sizeof(T) == 2) {
-      return *reinterpret_cast<const bf16x8*>(p + swz(r, kk * 2 + g) * 16);
+      return *reinterpret_cast<const bf16x8*>(t + (base ^ (uint32_t)(kk * 32)));
     } else {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(p + swz(r, kk * 4 + g * 2) * 16);
-      const f32x4 b = *reinterpret_cast<const f32x4*>(p + swz(r, kk * 4 + g * 2 + 1) * 16);
+      const f32x4 a = *reinterpret_cast<const f32x4*>(t + (base ^ (uint32_t)(kk * 64)));
+      const f32x4 b = *reinterpret_cast<const f32x4*>(t + (base ^ (uint32_t)(kk * 64 + 16)));
       frag f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -60,28 +69,34 @@ struct BothWays {
       return f;
     }
   }
-  // channel ch0 + lane % 32, rows r0 + 4 g + {0..3, 8..11}: the order in which a
-  // 32x32 result holds its rows
-  static __device__ __forceinline__ frag col(const char* t, int r0, int ch0, int lane) {
+  // Channels: 32 cb + lane % 32, rows 16 s + 4 (lane / 32) + {0..3, 8..11}, the
+  // order in which a 32x32 result holds its rows. In bf16 lane i of 16 addresses
+  // row i / 4 at channels 4 (i % 4) .. + 3 of the group's 16.
+  static __device__ __forceinline__ uint32_t col_base(int lane) {
     const int g = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+      const int r = g * 4 + ((lane & 15) >> 2), ch = (lane & 16) + 4 * (lane & 3);
+      return (uint32_t)(r * RB + swz(r, ch / 8) * 16 + ((ch / 4) & 1) * 8);
+    } else {
+      return (uint32_t)(g * 4 * RB + (((lane & 31) / 4) ^ (g * 4)) * 16 + (lane & 3) * 4);
+    }
+  }
+  static __device__ __forceinline__ frag col(const char* t, uint32_t base, int s, int cb) {
     frag f;
     if constexpr (sizeof(T) == 2) {
-      // lane i of 16 addresses row i / 4 at channels 4 (i % 4) .. + 3 of the group's 16
-      const int r = r0 + g * 4 + ((lane & 15) >> 2), ch = ch0 + (lane & 16) + 4 * (lane & 3);
-      auto at = [&](int k) { return t + k * RB + swz(k, ch / 8) * 16 + ((ch / 4) & 1) * 8; };
-      const auto a = __builtin_bit_cast(bf16x4, lds_read_tr16(at(r)));
-      const auto b = __builtin_bit_cast(bf16x4, lds_read_tr16(at(r + 8)));
+      const char* u = t + s * 16 * RB;
+      const auto a = __builtin_bit_cast(bf16x4, lds_read_tr16(u + (base ^ (uint32_t)(cb * 64))));
+      const auto b = __builtin_bit_cast(bf16x4, lds_read_tr16(u + 8 * RB + (base ^ (uint32_t)(cb * 64 + 32))));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         f[e] = a[e];
         f[e + 4] = b[e];
       }
     } else {
-      const int ch = ch0 + (lane & 31);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int r = r0 + (i / 4) * 8 + g * 4 + i % 4;
-        f[i] = *reinterpret_cast<const float*>(t + r * RB + swz(r, ch / 4) * 16 + (ch & 3) * 4);
+        const int r = (i / 4) * 8 + i % 4;
+        f[i] = *reinterpret_cast<const float*>(t + (s * 16 + r) * RB + (base ^ (uint32_t)(((cb * 8) ^ r) * 16)));
       }
     }
     return f;
@@ -118,13 +133,45 @@ struct BothWays {
   }
 };
 
-// Every XCD takes a contiguous run of the launch's workgroups, whose heads
-// share its L2.
-__device__ __forceinline__ int xcd_run() {
-  const int total = (int)gridDim.x, q = total / kNumXcd, rem = total % kNumXcd;
-  const int xcd = (int)blockIdx.x % kNumXcd, local = (int)blockIdx.x / kNumXcd;
-  return (xcd < rem ? xcd * (q + 1) : rem * (q + 1) + (xcd - rem) * q) + local;
+// Steps 0 .. N - 1 of a chain of matrix instructions, the operands of the next
+// one on their way from LDS while one runs (left alone, the compiler reads each
+// pair of operands where it is used and waits there).
+template <int N, class Load, class Use>
+__device__ __forceinline__ void pipelined(Load&& load, Use&& use) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i + 1 < N) load(i + 1, (i + 1) & 1);
+    __builtin_amdgcn_sched_barrier(0);
+    use(i, i & 1);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
+
+// The head and the item of this workgroup among `per_head` of each of `hk`
+// K/V heads, a launch of their product. Workgroups go to the XCDs in turn; a
+// head's items stay on as few XCDs as its share of them (their L2s hold its
+// rows), and every XCD gets every rank of them, heavy ones first. Runs of a
+// CU's number of workgroups go up and down the ranks in turn, so where all are
+// resident at once a heavy one shares a CU with a light one.
+struct Item {
+  int hk, at;
+  __device__ __forceinline__ Item(int hks, const FastDiv& fhk, int per_head) {
+    constexpr int kCus = 32;  // of an XCD
+    const int id = (int)blockIdx.x;
+    int i;
+    if (hks % kNumXcd == 0) {
+      const int local = id / kNumXcd;
+      const int round = local / per_head;
+      hk = round * kNumXcd + id % kNumXcd;
+      i = local - round * per_head;
+    } else {
+      i = fhk.div(id);
+      hk = id - i * hks;
+    }
+    const int row = i / kCus, n = min(per_head - row * kCus, kCus);
+    at = row & 1 ? row * kCus + n - 1 - (i - row * kCus) : i;
+  }
+};
 
 // The 128 columns (token, head of a K/V head's) of a workgroup: 32 per wave,
 // one per lane pair.
@@ -136,9 +183,10 @@ struct Columns {
   bool on;        // whether the lane has one
   int tok, head, row;
   __device__ __forceinline__ Columns(const PagedParams& p, int lane, int wave) {
-    const int blocks = (int)gridDim.x / p.hk, at = xcd_run();
-    hk = at / blocks;
-    const int blk = blocks - 1 - (at - hk * blocks);  // the columns that see most come first
+    const int blocks = (int)gridDim.x / p.hk;
+    const Item item(p.hk, p.fhk, blocks);
+    hk = item.hk;
+    const int blk = blocks - 1 - item.at;  // the columns that see most come first
     const int s = sequence_of_block<kPackedCols>(p, blk);
     sq.set(p, s);
     x0 = (blk - first_block<kPackedCols>(p, s)) * kPackedCols;

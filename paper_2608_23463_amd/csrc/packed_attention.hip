@@ -27,7 +27,8 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(PagedParams
   constexpr int kTileBytes = kRows * Tl::RB;
   __shared__ __attribute__((aligned(1024))) char smem[2][2 * kTileBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = lane >> 5, col = lane & 31;
+  const int g = lane >> 5;
+  const uint32_t rb = Tl::row_base(lane), cb0 = Tl::col_base(lane);
   const Columns c(p, lane, wave);
   if (!c.any) return;
   const Sight sight(p, c.sq, c.x0, c.cols, kRows);
@@ -68,7 +69,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(PagedParams
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.0f;
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) s = MM::mma(Tl::row(sk, col, kk, g), qf[kk], s);
+    for (int kk = 0; kk < D / 16; ++kk) s = MM::mma(Tl::row(sk, rb, kk), qf[kk], s);
     float top = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(PagedParams
     for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
       for (int cb = 0; cb < D / 32; ++cb)
-        o[cb] = MM::mma(Tl::col(sk + kTileBytes, s2 * 16, cb * 32, lane), Tl::operand(s, s2), o[cb]);
+        o[cb] = MM::mma(Tl::col(sk + kTileBytes, cb0, s2, cb), Tl::operand(s, s2), o[cb]);
   }
   if (!c.on) return;
   const float l = sum + other_half(sum), f = l > 0.0f ? 1.0f / l : l;

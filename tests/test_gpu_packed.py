@@ -279,7 +279,7 @@ def test_in_a_graph_and_on_another_stream(gpu, dtype):
     q, do = (torch.randn(300, 6, 64, device="cuda").to(dt) for _ in range(2))
     k, v = (torch.randn(300, 2, 64, device="cuda").to(dt) for _ in range(2))
     cu = torch.tensor([0, 100, 290], dtype=torch.int32, device="cuda")
-    ws = torch.empty(gpu.load().proxy_packed_workspace_size(cfg, 2, 300), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(gpu.load().proxy_packed_workspace_size(cfg, 2, 300, 300, 90, 2), dtype=torch.uint8, device="cuda")
 
     def both(ws=None, stream=None):
         out, lse = gpu.packed_attention_forward(cfg, q, k, v, cu, 300, window=90, sinks=2, stream=stream)

@@ -70,13 +70,15 @@ def test_packed_outputs_on_inputs():
 
 
 def test_packed_workspace():
-    need = B.load().proxy_packed_workspace_size(cfg(), 3, 5)
+    need = B.load().proxy_packed_workspace_size(cfg(), 3, 5, 5, 0, 0)
     assert need >= 8 * 5 * 8
     refused(backward(ws_bytes=need - 1), B.PF_ERR_WORKSPACE)
     refused(backward(ws=None), B.PF_ERR_WORKSPACE)
     refused(backward(ws=11 * P + 8))
     for bad in ((cfg(head_dim=96), 3, 5), (cfg(), 0, 5), (cfg(), 3, 0), (cfg(), 3, -1), (cfg(), 3, 1 << 40)):
-        assert B.load().proxy_packed_workspace_size(*bad) == 0
+        assert B.load().proxy_packed_workspace_size(*bad, 5, 0, 0) == 0
+    for bad in ((0, 0, 0), (5, -1, 0), (5, 0, -1)):
+        assert B.load().proxy_packed_workspace_size(cfg(), 3, 5, *bad) == 0
 
 
 def test_quant_cache_arguments():
