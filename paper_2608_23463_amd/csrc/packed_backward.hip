@@ -124,7 +124,7 @@ packed_dkdv_kernel(PagedParams p, PackedGrads z) {
   const int wk0 = k0 + wave * 32;
   int ih = b.first / b.tiles, it = b.first - ih * b.tiles, ct = it;  // head and tile of the loads, tile in turn
   auto issue = [&](int stage) {
-    const int q0 = k0 + it * kQueries, h = hk * p.group + ih;
+    const int q0 = k0 + (b.tiles - 1 - it) * kQueries, h = hk * p.group + ih;
     char* st = smem + stage * kStage;
     Tl::template load<kQueries>(p.q + (sq.t0 * p.q_ts + h * p.q_hs) * es, p.q_ts * es, q0, n - 1, st, wave, lane);
     Tl::template load<kQueries>(z.dout + (sq.t0 * z.do_ts + h * z.do_hs) * es, z.do_ts * es, q0, n - 1, st + kTileBytes,
@@ -143,7 +143,7 @@ packed_dkdv_kernel(PagedParams p, PackedGrads z) {
     wait_vmcnt<0>();
     lds_barrier();
     if (t + 1 < b.run) issue((t + 1) & 1);
-    const int q0 = k0 + ct * kQueries;
+    const int q0 = k0 + (b.tiles - 1 - ct) * kQueries;
     ct = ct + 1 == b.tiles ? 0 : ct + 1;
     // wave-uniform: nothing of the tile sees the wave's keys
     if (q0 + kQueries - 1 < wk0 || (q0 - p.window >= wk0 + 31 && wk0 >= p.sinks)) continue;
@@ -368,9 +368,16 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) packed_dq_ke
   store_rows<T, D>(reinterpret_cast<T*>(z.dq) + (c.sq.t0 + c.tok) * z.dq_ts + (int64_t)c.head * z.dq_hs, dq, z.scale, lane);
 }
 
-// How the queries of a block of keys are cut. Blocks near a sequence's start
-// are seen by most queries: where the blocks do not fill the chip several times
-// over, the longest would end alone.
+// How the queries of a block of keys are cut where the blocks do not fill the
+// chip: four workgroups per CU, of 8 tiles at least (two 128-key blocks of 300
+// tokens, 8 heads of 64, 31 us whole or in slices of 4), in fp32 two, of 2 (seven
+// documents of up to 500 tokens, window 100, 8 over 2 heads of 64: 96 us in slices of
+// 8, 80 of 2; 2,048 tokens, 16 over 4 heads of 128, 733 us, 917 in one per CU). Cuts that even out blocks of
+// different weight cost more in partial sums than they give (8 documents of up
+// to 4,096 tokens, 32 over 8 heads of 128, 1,088 blocks: 792 us whole, 810 in two
+// slices, 787 in up to four, and 23 and 56 us of joins; 8,192 tokens, 16 heads of
+// 64, 329 and 338, 348), and so does dealing them by weight over the documents
+// (907 us, their queries no longer shared in an L2).
 struct KeyPlan {
   int64_t groups;  // blocks of all heads
   int slices, min_tiles;
@@ -381,8 +388,8 @@ KeyPlan key_plan(const HeadsDims& d, int64_t n_tokens, int batch, int64_t max_le
   int64_t reach = std::min(max_len, n_tokens);
   if (window > 0 && sinks == 0) reach = std::min(reach, kKeys + std::min<int64_t>(window, INT32_MAX));
   const int64_t most = (reach + kQueries - 1) / kQueries * (d.hq / d.hk);  // tiles of a block
-  int64_t want = k.groups >= 4096 ? 1 : k.groups >= 2048 ? 2 : k.groups >= 512 ? 4 : (2048 + k.groups - 1) / k.groups;
-  k.min_tiles = k.groups >= 512 ? 64 : 8;
+  k.min_tiles = d.esize == 2 ? 8 : 2;
+  const int64_t want = k.groups >= 512 ? 1 : ((d.esize == 2 ? 1024 : 512) + k.groups - 1) / k.groups;
   k.slices = (int)std::max<int64_t>(1, std::min<int64_t>({want, most / k.min_tiles, 64}));
   return k;
 }

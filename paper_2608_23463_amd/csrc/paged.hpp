@@ -113,8 +113,12 @@ struct Sight {
 // packed rows in the order of the tokens.
 enum Source { kPages, kPages8, kPacked };
 
-// Factor of a scale byte, 2^(byte - 127) for bytes of 1 .. 254.
+// Factor of a scale byte, 2^(byte - 127) for bytes of 1 .. 254, and of the row
+// whose byte lies in a word of four rows'.
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+__device__ __forceinline__ float scale_in(uint32_t word, int row) {
+  return scale_of(__builtin_amdgcn_ubfe(word, (row & 3) * 8, 8));
+}
 
 // Two neighbouring e4m3 values, the lower or the upper half of a word, times a
 // power of two: exact in bf16 and in fp32.

@@ -179,16 +179,18 @@ struct Tile<float, D, false> {
 };
 
 // What rows of 8 bits share: a lane holds 16 channels of a row of K per load,
-// and of V the D / 16 neighbouring channels that it holds in bf16 too, so tiles
-// of four blocks are as many bytes as two in bf16. Values are widened where
-// they are used, times their row's power of two: exact in bf16 and fp32.
+// and of V the D / 16 neighbouring channels that it holds in bf16 too. Values are
+// widened where they are used, times their row's power of two: exact in bf16 and
+// fp32. Tiles of two blocks (48 sequences of up to 9,000 rows, 32 over 8 heads of
+// 128, 105 us, with four 144: their registers do not fit a third workgroup; 1M rows
+// 397 and 517; 32 sequences of 16,384 rows, 16 heads of 64, 209 and 209).
 template <int D>
 struct Raw8Tile {
   typedef uint8_t Stored;
-  static constexpr int NB = 4, KL = D / 64, VE = D / 16, JJ = 1, NO = VE;
+  static constexpr int NB = 2, KL = D / 64, VE = D / 16, JJ = 1, NO = VE;
   u32x4 k[NB][KL];
   uint32_t v[NB][4][VE / 4];
-  uint32_t ks[NB], vs[NB];  // the scale byte of the lane's row of K, four of its rows of V
+  uint32_t ks[NB], vs[NB];  // words with the scale byte of the lane's row of K, of its four rows of V
   __device__ __forceinline__ void load_k(int b, const uint8_t* row, int g) {
 #pragma unroll
     for (int s = 0; s < KL; ++s) k[b][s] = ld16(row + (4 * s + g) * 16);
@@ -207,7 +209,8 @@ struct Raw8Tile {
     for (int i = 0; i < VE / 4; ++i) v[b][r][i] = 0;
     vs[b] = (vs[b] & ~(255u << (8 * r))) | 127u << (8 * r);
   }
-  __device__ __forceinline__ float v_scale(int b, int r) const { return scale_of((vs[b] >> (8 * r)) & 255u); }
+  __device__ __forceinline__ float k_scale(int b) const { return scale_in(ks[b], (int)threadIdx.x); }
+  __device__ __forceinline__ float v_scale(int b, int r) const { return scale_in(vs[b], r); }
 };
 
 template <int D>
@@ -228,7 +231,7 @@ struct Tile<bf16, D, true> : Raw8Tile<D> {
   };
   __device__ __forceinline__ f32x4 scores(int b, const Query& q) const {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-    const float f = scale_of(ks[b]);
+    const float f = R::k_scale(b);
 #pragma unroll
     for (int i = 0; i < 2 * R::KL; ++i) {
       u32x4 a;
@@ -242,7 +245,7 @@ struct Tile<bf16, D, true> : Raw8Tile<D> {
     }
     return s;
   }
-  // (in two bf16 terms, as below the probabilities of a bf16 cache)
+  // (the probabilities in two bf16 terms, as for a bf16 cache)
   template <int E>  // channels E and E + 1 of the lane's
   __device__ __forceinline__ void pair(int c, const bf16x8& hi, const bf16x8& lo, f32x4* o) const {
     u32x4 a, z;
@@ -298,7 +301,7 @@ struct Tile<float, D, true> : Raw8Tile<D> {
   };
   __device__ __forceinline__ f32x4 scores(int b, const Query& q) const {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-    const float f = scale_of(ks[b]);
+    const float f = R::k_scale(b);
 #pragma unroll
     for (int i = 0; i < 4 * R::KL; ++i) {
       const uint32_t raw = k[b][i / 4][i % 4];
@@ -404,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<T, D, B8>::kPerCu)) paged_atte
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       t.load_k(b, kp + base(w, b) * D + m * D, g);
-      if constexpr (B8) t.ks[b] = p.k_scale[base(w, b) + m];
+      if constexpr (B8) t.ks[b] = *reinterpret_cast<const uint32_t*>(p.k_scale + base(w, b) + (m & ~3));
     }
   };
   auto fetch_v = [&](const Place& w) {
@@ -627,7 +630,7 @@ PagedPlan paged_plan(const HeadsDims& d, int batch, int64_t n_tokens, bool ragge
   PagedPlan pl;
   pl.prompt = d.esize == 2 && ragged && max_new >= kPromptTokens;
   pl.cols = pl.prompt ? 128 : kCols;
-  pl.tile_rows = pl.prompt ? 64 : kBlock * (bits8 ? 4 : d.esize == 4 && d.d == 128 ? 1 : 2);
+  pl.tile_rows = pl.prompt ? 64 : kBlock * (!bits8 && d.esize == 4 && d.d == 128 ? 1 : 2);
   window = std::min<int64_t>(window, INT32_MAX);
   sinks = std::min<int64_t>(sinks, INT32_MAX);
   max_new = std::min<int64_t>(max_new, n_tokens);

@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
   // bf16 cache (a power of two times e4m3 is exact in bf16).
   constexpr int C8 = D / 16, kLoads8 = kBlock * C8 / kWave, kRows8 = kWave / C8;
   u32x4 raw_k[kLoads8], raw_v[kLoads8];
-  uint32_t byte_k[kLoads8], byte_v[kLoads8];
+  uint32_t word_k[kLoads8], word_v[kLoads8];  // with the row's scale byte (a loaded byte would be waited for to be widened)
   auto fetch8 = [&](int t, int rows, int at) {
     const int r0 = tile_row(t);
     const int mine16 = __builtin_amdgcn_readlane(rows, at + wave);
@@ -160,8 +160,8 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
       const bool none = !all && unseen(r0 + wave * kBlock + r);
       raw_k[j] = buf_ld16(rk, (uint32_t)(r * D + c * 16));
       raw_v[j] = buf_ld16(rv, none ? kOOB : (uint32_t)(r * D + c * 16));
-      byte_k[j] = __builtin_amdgcn_raw_buffer_load_b8(sk, r, 0, 0);
-      byte_v[j] = __builtin_amdgcn_raw_buffer_load_b8(sv, none ? kOOB : (uint32_t)r, 0, 0);
+      word_k[j] = __builtin_amdgcn_raw_buffer_load_b32(sk, r & ~3, 0, 0);
+      word_v[j] = __builtin_amdgcn_raw_buffer_load_b32(sv, none ? kOOB : (uint32_t)(r & ~3), 0, 0);
     }
   };
   auto put8 = [&](int stage) {
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
 #pragma unroll
     for (int j = 0; j < kLoads8; ++j) {
       const int r = wave * kBlock + j * kRows8 + lane / C8, c = lane % C8;
-      const float fk = scale_of(byte_k[j]), fv = scale_of(byte_v[j]);
+      const float fk = scale_in(word_k[j], r), fv = scale_in(word_v[j], r);
       u32x4 k[2], v[2];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
