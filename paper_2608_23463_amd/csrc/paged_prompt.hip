@@ -234,8 +234,13 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
     if constexpr (FROM == kPages8) {
       fetch8(0, rows, 0);
       put8(0);
-      if (ntiles > 1) fetch8(1, rows, kPerTile);
     }
+  }
+  if constexpr (FROM == kPages8) {
+    // the queries and table entries are there too, whatever the way here: else the
+    // loop would wait for them, and with them for the rows on their way
+    wait_vmcnt<0>();
+    if (ntiles > 1) fetch8(1, rows, kPerTile);
   }
   for (int t = 0; t < ntiles; ++t) {
     const int r0 = tile_row(t), in = t % kAhead;
@@ -329,11 +334,15 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
     };
     float tsum = 0.0f;
     bool redo = !have_ref;
-    bf16x8 early[D / 32];  // of the first 16 rows, read while the exponentials are taken
+    // of the first 16 rows, read while the exponentials are taken (rows of 8 bits on
+    // their way take these registers)
+    constexpr bool kEarly = FROM != kPages8;
+    bf16x8 early[kEarly ? D / 32 : 1];
     auto products = [&]() {
       scores();
+      if constexpr (kEarly)
 #pragma unroll
-      for (int cb = 0; cb < D / 32; ++cb) early[cb] = values(0, 0, cb);
+        for (int cb = 0; cb < D / 32; ++cb) early[cb] = values(0, 0, cb);
     };
     if (have_ref && whole) {  // one run of instructions: products, reads and exponentials side by side
       products();
@@ -393,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
         const bf16x8 pb = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
         for (int cb = 0; cb < D / 32; ++cb)
-          o[cb] = Mma<bf16>::mma(kb == 0 && s2 == 0 ? early[cb] : values(kb, s2, cb), pb, o[cb]);
+          o[cb] = Mma<bf16>::mma(kEarly && kb == 0 && s2 == 0 ? early[kEarly ? cb : 0] : values(kb, s2, cb), pb, o[cb]);
       }
     __builtin_amdgcn_s_setprio(0);
   }
