@@ -70,13 +70,12 @@ __device__ __forceinline__ int find_run(int count, F&& at, int64_t x) {
   return __builtin_amdgcn_readfirstlane(s);
 }
 
-// Where token `tok` of a call is in a cache: its row (head 0) in the pages, or -1
-// for one of no sequence or without a place; `at` is its row of the sequence,
-// kv_len - new + i for the i-th new token.
-__device__ __forceinline__ int64_t cache_place(const int32_t* cu, const int32_t* kv_len, const int32_t* table, int batch,
-                                               int max_pages, int n_pages, int hk, const FastDiv& fpage, int64_t tok,
-                                               int* at) {
-  const int s = cu ? find_run(batch + 1, [&](int c) { return cu[c]; }, tok) : (int)tok;
+// Where token `tok` of a call, of sequence s, is in a cache: its row (head 0) in
+// the pages, or -1 for one of no sequence or without a place; `at` is its row of
+// the sequence, kv_len - new + i for the i-th new token.
+__device__ __forceinline__ int64_t place_in(const int32_t* cu, const int32_t* kv_len, const int32_t* table, int batch,
+                                            int max_pages, int n_pages, int hk, const FastDiv& fpage, int64_t tok, int s,
+                                            int* at) {
   *at = 0;
   if (s >= batch || (cu && tok < cu[s])) return -1;
   const int64_t pos = cu ? (int64_t)kv_len[s] - cu[s + 1] + tok : (int64_t)kv_len[s] - 1;
@@ -87,6 +86,13 @@ __device__ __forceinline__ int64_t cache_place(const int32_t* cu, const int32_t*
   return id >= 0 && id < n_pages ? (int64_t)id * hk * fpage.d + ((int)pos - pg * fpage.d) : -1;
 }
 
+// The same, with its sequence to be found (by the whole wave).
+__device__ __forceinline__ int64_t cache_place(const int32_t* cu, const int32_t* kv_len, const int32_t* table, int batch,
+                                               int max_pages, int n_pages, int hk, const FastDiv& fpage, int64_t tok,
+                                               int* at) {
+  return place_in(cu, kv_len, table, batch, max_pages, n_pages, hk, fpage, tok,
+                  cu ? find_run(batch + 1, [&](int c) { return cu[c]; }, tok) : (int)tok, at);
+}
 int heads_dims(const pf_heads_config* c, HeadsDims* d, const char** why);
 
 // Forward: q -> q_out, k -> k_out. n_tokens rows, positions [n_axes, n_tokens].

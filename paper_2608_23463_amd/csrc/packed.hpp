@@ -173,46 +173,6 @@ struct Item {
   }
 };
 
-// Sum over the wave, in every lane.
-__device__ __forceinline__ int wave_sum(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // row_shr 1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);  // row_bcast 15, 31
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);
-  return __builtin_amdgcn_readlane(v, kWave - 1);
-}
-
-// The r-th block of up to 64 sequences by its number from its sequence's end
-// (`level`, from 1), the highest first: heavy blocks of all sequences before
-// light ones. Sequence s has count(s) of them. seq < 0: there are no more.
-struct Ranked {
-  int seq, level;
-  template <class F>
-  __device__ __forceinline__ Ranked(int r, int batch, int most, F&& count) {
-    const int lane = (int)(threadIdx.x & (kWave - 1));
-    const int c = lane < batch ? count(lane) : 0;
-    auto from = [&](int l) { return wave_sum(max(c - l + 1, 0)); };  // blocks of level l and more
-    seq = -1;
-    if (from(1) <= r) return;
-    int lo = 1, hi = most + 1;  // from(lo) > r, from(hi) <= r
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (from(mid) > r)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    level = lo;
-    uint64_t have = __builtin_amdgcn_ballot_w64(c >= lo);
-    for (int i = r - from(lo + 1); i > 0; --i) have &= have - 1;
-    seq = __builtin_ctzll(have);
-  }
-};
-// Launches that fill the chip are ranked so; others are all resident at once.
-constexpr int kRankedGroups = 512;
-
 // The 128 columns (token, head of a K/V head's) of a workgroup: 32 per wave,
 // one per lane pair.
 constexpr int kPackedCols = 128;
@@ -227,15 +187,11 @@ struct Columns {
     const Item item(p.hk, p.fhk, blocks);
     hk = item.hk;
     // the columns that see most come first
-    if (p.batch <= kWave && (int)gridDim.x >= kRankedGroups) {
-      const Ranked r(item.at, p.batch, blocks, [&](int s) {
-        Sequence x;
-        x.set(p, s);
-        return x.seq < 0 ? 0 : (x.cols + kPackedCols - 1) / kPackedCols;
-      });
+    if (ranked(p, (int)gridDim.x)) {
+      const Ranked r(item.at, p.batch, kPackedCols, p);
       any = r.seq >= 0;
       sq.set(p, any ? r.seq : 0);
-      x0 = any ? (r.level - 1) * kPackedCols : 0;
+      x0 = any ? r.block * kPackedCols : 0;
     } else {
       const int blk = blocks - 1 - item.at, s = sequence_of_block<kPackedCols>(p, blk);
       sq.set(p, s);

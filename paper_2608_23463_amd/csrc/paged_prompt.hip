@@ -56,12 +56,22 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
     at = (xcd < rem ? xcd * (q + 1) : rem * (q + 1) + (xcd - rem) * q) + local;
   }
   const int unit = p.fslices.div(at), slice = at - unit * p.slices;
-  const int hk = unit / blocks, blk = blocks - 1 - (unit - hk * blocks);
-  const int s = sequence_of_block<kColumns>(p, blk);
+  const int hk = unit / blocks, rank = unit - hk * blocks;
   Sequence sq;
-  sq.set(p, s);
-  const int x0 = (blk - first_block<kColumns>(p, s)) * kColumns;
-  if (sq.seq < 0 || x0 < 0 || x0 >= sq.cols) return;
+  int s, x0;
+  if (ranked(p, total)) {
+    const Ranked r(rank, p.batch, kColumns, p);
+    if (r.seq < 0) return;
+    s = r.seq;
+    sq.set(p, s);
+    x0 = r.block * kColumns;
+  } else {
+    const int blk = blocks - 1 - rank;
+    s = sequence_of_block<kColumns>(p, blk);
+    sq.set(p, s);
+    x0 = (blk - first_block<kColumns>(p, s)) * kColumns;
+    if (sq.seq < 0 || x0 < 0 || x0 >= sq.cols) return;
+  }
   const int cols = min(sq.cols - x0, kColumns);
   const Sight sight(p, sq, x0, cols, kTile);
   const int per = sight.per_slice(p);

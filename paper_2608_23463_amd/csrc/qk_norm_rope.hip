@@ -188,8 +188,15 @@ template <int CTRL>
 __device__ __forceinline__ float add_lane(float v) {
   return v + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-template <int LPR>
-__device__ __forceinline__ float row_sum(float v) {
+template <int CTRL>
+__device__ __forceinline__ double add_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
+  return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int LPR, typename V>
+__device__ __forceinline__ V row_sum(V v) {
   static_assert(LPR == 4 || LPR == 8, "lanes of a row");
   v = add_lane<0xb1>(v);              // quad_perm 1 0 3 2
   v = add_lane<0x4e>(v);              // quad_perm 2 3 0 1
@@ -248,11 +255,38 @@ __device__ __forceinline__ void load_gain(const QkParams& p, const Tensor& x, in
   }
 }
 
-// Norm and rotation of the lane's 16 elements of a row.
-template <int D, bool PAIRS>
+// What a launch does with the rows: turned ones to tensors, or keys and values
+// into pages of the rows' type or of 8 bits.
+enum Mode { kTurn, kAppend, kAppend8 };
+
+// Norm and rotation of the lane's 16 elements of a row. FINE: for rows that are
+// held in 8 bits, whose values next to a border every rounding on the way moves
+// by a whole step: the norm in 64 bits (keys are few beside queries), one
+// rounding for each product of the turn.
+template <int D, bool PAIRS, bool FINE>
 __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, float* v, const float* g, const float2* cs,
                                               bool turned) {
   if (which == 2) return;
+  if (FINE && which == 1) {
+    if (p.norm) {
+      double ss = 0.0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ss += (double)v[i] * v[i];
+      const double m = row_sum<D / 16>(ss) * (1.0 / D) + p.eps;
+      double r = rsqrtf((float)m);
+      r *= 1.5 - 0.5 * m * r * r;  // of 2^-23 of the root 2^-45
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = (float)(v[i] * r * g[i]);
+    }
+    if (turned)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double a = v[ia<PAIRS>(i)], b = v[ib<PAIRS>(i)], c = cs[i].x, s = cs[i].y;
+        v[ia<PAIRS>(i)] = (float)(a * c - b * s);
+        v[ib<PAIRS>(i)] = (float)(a * s + b * c);
+      }
+    return;
+  }
   if (p.norm) {
     float ss = 0.0f;
 #pragma unroll
@@ -269,10 +303,6 @@ __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, floa
 __device__ __forceinline__ int64_t place_of(const QkParams& p, int64_t tok, int* at) {
   return cache_place(p.cu, p.kv_len, p.table, p.batch, p.max_pages, p.n_pages, p.hk, p.fpage, tok, at);
 }
-
-// What a launch does with the rows: turned ones to tensors, or keys and values
-// into pages of the rows' type or of 8 bits.
-enum Mode { kTurn, kAppend, kAppend8 };
 
 // The lane's 16 elements of a row, turned, to their place: tensors, or pages
 // where `place` is the token's row.
@@ -367,7 +397,7 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p) {
       load16(reinterpret_cast<const T*>(x.in.p) + (t0 + tk) * x.in.ts + h * x.in.hs, ch.a, ch.b, r);
       raw_to_f32(r[0], v);
       raw_to_f32(r[1], v + 8);
-      norm_and_turn<D, PAIRS>(p, which, v, g, &turns[wave][tk][8 * (lane % LPR)], ch.turned);
+      norm_and_turn<D, PAIRS, MODE == kAppend8>(p, which, v, g, &turns[wave][tk][8 * (lane % LPR)], ch.turned);
       const int64_t place = APPEND ? places[wave][tk] : 0;
       put_row<T, D, MODE>(p, x, t0 + tk, h, on && place >= 0, place, ch.a, ch.b, v);
     }
@@ -412,7 +442,7 @@ __global__ void __launch_bounds__(kThreads) qk_few_kernel(QkParams p) {
   }
   raw_to_f32(r[0], v);
   raw_to_f32(r[1], v + 8);
-  norm_and_turn<D, PAIRS>(p, which, v, g, &turns[wave][8 * (lane % LPR)], ch.turned);
+  norm_and_turn<D, PAIRS, MODE == kAppend8>(p, which, v, g, &turns[wave][8 * (lane % LPR)], ch.turned);
   put_row<T, D, MODE>(p, x, tok, h, on && place >= 0, place, ch.a, ch.b, v);
 }
 
