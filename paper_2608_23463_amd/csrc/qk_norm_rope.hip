@@ -259,10 +259,11 @@ __device__ __forceinline__ void load_gain(const QkParams& p, const Tensor& x, in
 // into pages of the rows' type or of 8 bits.
 enum Mode { kTurn, kAppend, kAppend8 };
 
-// Norm and rotation of the lane's 16 elements of a row. FINE: for rows that are
-// held in 8 bits, whose values next to a border every rounding on the way moves
-// by a whole step: the norm in 64 bits (keys are few beside queries), one
-// rounding for each product of the turn.
+// Norm and rotation of the lane's 16 elements of a row. FINE: in 64 bits, for
+// keys that are held in 8, whose values next to a border each error on the way
+// moves by a whole step. Element after element: side by side the products would
+// cost the registers of a workgroup (24 prompts of up to 2,600 tokens, 32 over 8
+// heads of 128, 190 us for 163, 152 in 32 bits).
 template <int D, bool PAIRS, bool FINE>
 __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, float* v, const float* g, const float2* cs,
                                               bool turned) {
@@ -271,12 +272,20 @@ __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, floa
     if (p.norm) {
       double ss = 0.0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ss += (double)v[i] * v[i];
+      for (int i = 0; i < 16; ++i) {
+        ss += (double)v[i] * v[i];
+        asm volatile("" : "+v"(ss));
+      }
       const double m = row_sum<D / 16>(ss) * (1.0 / D) + p.eps;
       double r = rsqrtf((float)m);
       r *= 1.5 - 0.5 * m * r * r;  // of 2^-23 of the root 2^-45
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = (float)(v[i] * r * g[i]);
+      for (int i = 0; i < 16; ++i) {
+        float gain = g[i];
+        asm volatile("" : "+v"(gain));  // widened here, not kept wide over the rows
+        v[i] = (float)(v[i] * r * gain);
+        asm volatile("" : "+v"(v[i]));
+      }
     }
     if (turned)
 #pragma unroll
@@ -284,6 +293,7 @@ __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, floa
         const double a = v[ia<PAIRS>(i)], b = v[ib<PAIRS>(i)], c = cs[i].x, s = cs[i].y;
         v[ia<PAIRS>(i)] = (float)(a * c - b * s);
         v[ib<PAIRS>(i)] = (float)(a * s + b * c);
+        asm volatile("" : "+v"(v[ia<PAIRS>(i)]), "+v"(v[ib<PAIRS>(i)]));
       }
     return;
   }
