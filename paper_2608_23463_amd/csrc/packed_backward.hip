@@ -250,14 +250,14 @@ __global__ void __launch_bounds__(kThreads) packed_join_kernel(PagedParams p, Pa
 // scores' gradients where a query sees few keys. But these add up to zero over
 // a query's keys, so what they add up to corrects D: for the kernel of dK and dV,
 // which runs behind this one, and where a workgroup sees few tiles for dQ too.
-constexpr int kFewTiles = 8;
+constexpr int kFewTiles = 4;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) packed_dq_kernel(PagedParams p, PackedGrads z) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? (D == 64 ? 3 : 2) : 1) packed_dq_kernel(PagedParams p, PackedGrads z) {
   constexpr bool kCorrect = sizeof(T) == 2;
   typedef BothWays<T, D> Tl;
   typedef Mma<T> MM;
-  constexpr int kRows = 32, kTileBytes = kRows * Tl::RB, es = (int)sizeof(T);
+  constexpr int kRows = sizeof(T) == 2 ? 64 : 32, kTileBytes = kRows * Tl::RB, es = (int)sizeof(T);
   __shared__ __attribute__((aligned(1024))) char smem[2][2 * kTileBytes];  // K, V
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5;
@@ -315,52 +315,55 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) packed_dq_ke
       st.y += slip + other_half(slip);
       slip = 0.0f;
     }
-    const int r0 = tile_row(t);
-    if (r0 > wtop || (r0 + kRows - 1 <= wfirst - p.window && r0 >= p.sinks)) continue;  // wave-uniform
     const char* sk = smem[t & 1];
     const char* sv = sk + kTileBytes;
-    f32x16 sc, dp;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = dp[r] = 0.0f;
-    typename MM::frag fa[2], fb[2];
-    auto rows_of = [&](int kk, int u) {
-      fa[u] = Tl::row(sk, rb, kk);
-      fb[u] = Tl::row(sv, rb, kk);
-    };
-    auto cols_of = [&](int i, int u) { fa[u] = Tl::col(sk, cb0, i / (D / 32), i % (D / 32)); };
-    __builtin_amdgcn_s_setprio(1);
-    rows_of(0, 0);
-    pipelined<D / 16>(rows_of, [&](int kk, int u) {
-      sc = MM::mma(fa[u], qf[kk], sc);
-      dp = MM::mma(fb[u], of[kk], dp);
-    });
-    __builtin_amdgcn_s_setprio(0);
-    cols_of(0, 0);
-    const bool whole = r0 + kRows - 1 <= wfirst && (r0 > wtop - p.window || r0 + kRows <= p.sinks);
+    for (int kb = 0; kb < kRows / 32; ++kb) {
+      const int r0 = tile_row(t) + kb * 32;
+      if (r0 > wtop || (r0 + 31 <= wfirst - p.window && r0 >= p.sinks)) continue;  // wave-uniform
+      f32x16 sc, dp;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = fast_exp2(fmaf(sc[r], p.scale_log2, -st.x)) * (dp[r] - st.y);
-    if (!whole) {
+      for (int r = 0; r < 16; ++r) sc[r] = dp[r] = 0.0f;
+      typename MM::frag fa[2], fb[2];
+      auto rows_of = [&](int kk, int u) {
+        fa[u] = Tl::row(sk + kb * 32 * Tl::RB, rb, kk);
+        fb[u] = Tl::row(sv + kb * 32 * Tl::RB, rb, kk);
+      };
+      auto cols_of = [&](int i, int u) { fa[u] = Tl::col(sk + kb * 32 * Tl::RB, cb0, i / (D / 32), i % (D / 32)); };
+      __builtin_amdgcn_s_setprio(1);
+      rows_of(0, 0);
+      pipelined<D / 16>(rows_of, [&](int kk, int u) {
+        sc = MM::mma(fa[u], qf[kk], sc);
+        dp = MM::mma(fb[u], of[kk], dp);
+      });
+      __builtin_amdgcn_s_setprio(0);
+      cols_of(0, 0);
+      const bool whole = r0 + 31 <= wfirst && (r0 > wtop - p.window || r0 + 32 <= p.sinks);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = r0 + acc_row(r, lane);
-        const bool sees = (j <= c.row) & ((j > lo) | (j < p.sinks));
-        sc[r] = sees ? sc[r] : 0.0f;
+      for (int r = 0; r < 16; ++r) sc[r] = fast_exp2(fmaf(sc[r], p.scale_log2, -st.x)) * (dp[r] - st.y);
+      if (!whole) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = r0 + acc_row(r, lane);
+          const bool sees = (j <= c.row) & ((j > lo) | (j < p.sinks));
+          sc[r] = sees ? sc[r] : 0.0f;
+        }
       }
-    }
-    if (kCorrect) {
-      float add[4] = {};
+      if (kCorrect) {
+        float add[4] = {};
 #pragma unroll
-      for (int r = 0; r < 16; ++r) add[r & 3] += sc[r];
-      slip += (add[0] + add[1]) + (add[2] + add[3]);
+        for (int r = 0; r < 16; ++r) add[r & 3] += sc[r];
+        slip += (add[0] + add[1]) + (add[2] + add[3]);
+        if (t < last_pass) continue;
+      }
+      const typename MM::frag df[2] = {Tl::operand(sc, 0), Tl::operand(sc, 1)};
+      __builtin_amdgcn_s_setprio(1);
+      pipelined<D / 16>(cols_of, [&](int i, int u) {
+        const int cb = i % (D / 32);
+        dq[cb] = MM::mma(fa[u], df[i / (D / 32)], dq[cb]);
+      });
+      __builtin_amdgcn_s_setprio(0);
     }
-    if (kCorrect && t < last_pass) continue;
-    const typename MM::frag df[2] = {Tl::operand(sc, 0), Tl::operand(sc, 1)};
-    __builtin_amdgcn_s_setprio(1);
-    pipelined<D / 16>(cols_of, [&](int i, int u) {
-      const int cb = i % (D / 32);
-      dq[cb] = MM::mma(fa[u], df[i / (D / 32)], dq[cb]);
-    });
-    __builtin_amdgcn_s_setprio(0);
   }
   slip += other_half(slip);
   if (!c.on) return;
