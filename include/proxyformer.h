@@ -564,8 +564,9 @@ int proxy_packed_attention_forward(const pf_heads_config* cfg, int32_t batch, in
  * forward's out and lse; dk and dv are summed over the query heads that share
  * a key/value head. Every gradient is summed in fp32 in a fixed order and
  * rounded once; in bf16 the weights and the scores' gradients are rounded to
- * bf16 in their products. Tokens behind the last sequence are left as they
- * were. dq, dk and dv overlap neither each other nor what the call reads; they
+ * bf16 in their products. What is not finite reaches other tokens as in the
+ * forward, and from a token's dout and q the gradients of earlier rows whose
+ * tiles it is in. Tokens behind the last sequence are left as they were. dq, dk and dv overlap neither each other nor what the call reads; they
  * may be bands of one buffer. workspace: proxy_packed_workspace_size bytes
  * (0 for invalid sizes), 16-byte aligned, overlapping nothing else; calls that
  * may run at the same time need workspaces of their own. */

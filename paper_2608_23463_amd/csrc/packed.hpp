@@ -116,10 +116,11 @@ struct BothWays {
     }
   }
   // Wave `wave`'s share of the loads of rows j0 .. j0 + ROWS - 1 of a tensor
-  // whose row 0 is at `base`, strides in bytes; rows past `last` land as zeros.
+  // whose row 0 is at `base`, strides in bytes; rows past `last` land as zeros,
+  // and so do those up to `before` from `sinks` on.
   template <int ROWS>
   static __device__ __forceinline__ void load(const char* base, int64_t stride, int j0, int last, char* tile, int wave,
-                                              int lane) {
+                                              int lane, int before = -1, int sinks = 0) {
     constexpr int kPer = ROWS * RB / 4096, kRows = 1024 / RB;
     static_assert(kPer >= 1, "every wave loads");
     const rsrc_t rs = make_rsrc_uniform(base + (int64_t)j0 * stride, kOOB - 1);
@@ -127,7 +128,7 @@ struct BothWays {
     for (int j = 0; j < kPer; ++j) {
       const int i = wave * kPer + j, r = i * kRows + lane / CH;
       uint32_t off = (uint32_t)(r * (int)stride + swz(r, lane % CH) * 16);
-      if (j0 + r > last) off = kOOB;
+      if (j0 + r > last || (j0 + r <= before && j0 + r >= sinks)) off = kOOB;
       buf_ld16_lds(rs, off, tile + i * 1024);
     }
   }

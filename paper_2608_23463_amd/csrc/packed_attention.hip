@@ -49,7 +49,8 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(PagedParams
   auto issue = [&](int t) {
     const int r0 = sight.tile(t) * kRows;
     Tl::template load<kRows>(k, p.k_ts * 4, r0, sight.last, smem[t & 1], wave, lane);
-    Tl::template load<kRows>(v, p.v_ts * 4, r0, sight.last, smem[t & 1] + kTileBytes, wave, lane);
+    Tl::template load<kRows>(v, p.v_ts * 4, r0, sight.last, smem[t & 1] + kTileBytes, wave, lane, sight.first - p.window,
+                             p.sinks);
   };
   f32x16 o[D / 32];
 #pragma unroll

@@ -45,7 +45,8 @@ struct KeyBlock {
   bool any;
   Sequence sq;
   int hk, blk, s, n, k0;
-  int tiles;       // of queries that see one of the keys, per head
+  int last;        // the last query that sees one of the keys
+  int tiles;       // of the queries up to it, per head
   int run, first;  // tiles of a slice, the first of this one
   int live;        // slices that have any
   // `slice`: the workgroup's, of z.slices
@@ -60,7 +61,8 @@ struct KeyBlock {
     // the queries that see a key of the block: from its first key on, up to the
     // end of its last key's windows, or to the sequence's end for the first rows
     const int64_t reach = k0 < p.sinks ? n : min((int64_t)n, (int64_t)k0 + kKeys - 1 + p.window);
-    tiles = ((int)reach - k0 + kQueries - 1) / kQueries;
+    last = (int)reach - 1;
+    tiles = (last - k0) / kQueries + 1;
     const int all = tiles * p.group, cut = max(min(z.fmin_tiles.div(all), z.slices), 1);
     run = (all + cut - 1) / cut;
     live = (all + run - 1) / run;
@@ -126,8 +128,8 @@ packed_dkdv_kernel(PagedParams p, PackedGrads z) {
   auto issue = [&](int stage) {
     const int q0 = k0 + (b.tiles - 1 - it) * kQueries, h = hk * p.group + ih;
     char* st = smem + stage * kStage;
-    Tl::template load<kQueries>(p.q + (sq.t0 * p.q_ts + h * p.q_hs) * es, p.q_ts * es, q0, n - 1, st, wave, lane);
-    Tl::template load<kQueries>(z.dout + (sq.t0 * z.do_ts + h * z.do_hs) * es, z.do_ts * es, q0, n - 1, st + kTileBytes,
+    Tl::template load<kQueries>(p.q + (sq.t0 * p.q_ts + h * p.q_hs) * es, p.q_ts * es, q0, b.last, st, wave, lane);
+    Tl::template load<kQueries>(z.dout + (sq.t0 * z.do_ts + h * z.do_hs) * es, z.do_ts * es, q0, b.last, st + kTileBytes,
                                 wave, lane);
     if (wave == 0) {
       const rsrc_t rs = make_rsrc_uniform(z.stats + h * z.stat_rows + stat_row(sq.t0, b.s) + q0, kQueries * 8);
@@ -145,8 +147,8 @@ packed_dkdv_kernel(PagedParams p, PackedGrads z) {
     if (t + 1 < b.run) issue((t + 1) & 1);
     const int q0 = k0 + (b.tiles - 1 - ct) * kQueries;
     ct = ct + 1 == b.tiles ? 0 : ct + 1;
-    // wave-uniform: nothing of the tile sees the wave's keys
-    if (q0 + kQueries - 1 < wk0 || (q0 - p.window >= wk0 + 31 && wk0 >= p.sinks)) continue;
+    // wave-uniform: the wave has no keys, or nothing of the tile sees them
+    if (wk0 >= n || q0 + kQueries - 1 < wk0 || (q0 - p.window >= wk0 + 31 && wk0 >= p.sinks)) continue;
     const char* sq_ = smem + (t & 1) * kStage;
     const char* so = sq_ + kTileBytes;
     const float* st = reinterpret_cast<const float*>(so + kTileBytes);
@@ -294,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? (D == 64 ? 3 : 2) :
   auto tile_row = [&](int t) { return sight.tile(t < sight.tiles ? t : t - sight.tiles) * kRows; };
   auto issue = [&](int t) {
     const int r0 = tile_row(t);
-    Tl::template load<kRows>(k, p.k_ts * es, r0, sight.last, smem[t & 1], wave, lane);
+    Tl::template load<kRows>(k, p.k_ts * es, r0, sight.last, smem[t & 1], wave, lane, sight.first - p.window, p.sinks);
     Tl::template load<kRows>(v, p.v_ts * es, r0, sight.last, smem[t & 1] + kTileBytes, wave, lane);
   };
   f32x16 dq[D / 32];
@@ -372,15 +374,17 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? (D == 64 ? 3 : 2) :
 }
 
 // How the queries of a block of keys are cut where the blocks do not fill the
-// chip: four workgroups per CU, of 8 tiles at least (two 128-key blocks of 300
-// tokens, 8 heads of 64, 31 us whole or in slices of 4), in fp32 two, of 2 (seven
-// documents of up to 500 tokens, window 100, 8 over 2 heads of 64: 96 us in slices of
-// 8, 80 of 2; 2,048 tokens, 16 over 4 heads of 128, 733 us, 917 in one per CU). Cuts that even out blocks of
-// different weight cost more in partial sums than they give (8 documents of up
-// to 4,096 tokens, 32 over 8 heads of 128, 1,088 blocks: 792 us whole, 810 in two
-// slices, 787 in up to four, and 23 and 56 us of joins; 8,192 tokens, 16 heads of
-// 64, 329 and 338, 348), and so does dealing them by weight over the documents
-// (907 us, their queries no longer shared in an L2).
+// chip: four workgroups per CU, of 8 tiles at least, 4 where they are few (two of
+// up to 200 tokens, 8 over 2 heads of 128, 32 us for 42; 2,048 tokens, 32 over 8 heads
+// of 128, 169 us, 352 whole, 208 in half as many of 32; 8,192 tokens, 4 heads of 64,
+// 241, 378 and 272), in fp32 two, of 2 (seven documents of up to 500 tokens, window
+// 100, 8 over 2 heads of 64: 96 us in slices of 8, 80 of 2). From one round of
+// workgroups on, two slices of long lists (8,192 tokens, 32 over 8 heads of 128, 1,908
+// us, 2,064 whole). Of several rounds, cuts cost more in partial sums than they even
+// out (8 documents of up to 4,096 tokens, 32 over 8 heads of 128, 1,000 blocks: 792 us
+// whole, 810 in two slices, 787 in up to four, and 23 and 56 us of joins; 8,192 tokens,
+// 16 heads of 64, 329 and 338, 348), and so does dealing them by weight over the
+// documents (907 us, their queries no longer shared in an L2).
 struct KeyPlan {
   int64_t groups;  // blocks of all heads
   int slices, min_tiles;
@@ -391,8 +395,9 @@ KeyPlan key_plan(const HeadsDims& d, int64_t n_tokens, int batch, int64_t max_le
   int64_t reach = std::min(max_len, n_tokens);
   if (window > 0 && sinks == 0) reach = std::min(reach, kKeys + std::min<int64_t>(window, INT32_MAX));
   const int64_t most = (reach + kQueries - 1) / kQueries * (d.hq / d.hk);  // tiles of a block
-  k.min_tiles = d.esize == 2 ? 8 : 2;
-  const int64_t want = k.groups >= 512 ? 1 : ((d.esize == 2 ? 1024 : 512) + k.groups - 1) / k.groups;
+  const bool wide = d.esize == 2;
+  k.min_tiles = k.groups >= 512 ? 128 : !wide ? 2 : k.groups < 64 ? 4 : 8;
+  const int64_t want = k.groups >= 768 ? 1 : k.groups >= 512 ? 2 : ((wide ? 1024 : 512) + k.groups - 1) / k.groups;
   k.slices = (int)std::max<int64_t>(1, std::min<int64_t>({want, most / k.min_tiles, 64}));
   return k;
 }

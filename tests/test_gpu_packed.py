@@ -199,6 +199,39 @@ def test_other_sequences_and_the_space_behind(gpu, dtype, window):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_windows_leave_behind(gpu, dtype, d):
+    """Infinities and NaNs in rows that windows of 50 have left reach neither
+    results nor gradients of tokens 128 (a workgroup's) and more past the last
+    that sees them, first rows in sight or not; nor, on the way back, those of
+    tokens 128 and more before them."""
+    import torch
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    cfg = gpu.heads_config(4, 2, d, dtype=dtype, norm=False, rot_dim=0)
+    cu = torch.tensor([0, 700], dtype=torch.int32, device="cuda")
+    torch.manual_seed(6)
+    x = [torch.randn(700, h, d, device="cuda").to(dt) for h in (4, 2, 2, 4)]
+    for sinks in (0, 3):
+        def both():
+            q, k, v, do = x
+            out, lse = gpu.packed_attention_forward(cfg, q, k, v, cu, 700, window=50, sinks=sinks)
+            return out, *gpu.packed_attention_backward(cfg, q, k, v, out, lse, do, cu, 700, window=50, sinks=sinks)
+
+        clean = both()
+        keep = [y.clone() for y in x]
+        for y in x:
+            y[300:310] = float("nan")
+            y[305] = float("inf")
+        got = both()
+        for y, z in zip(x, keep):
+            y.copy_(z)
+        for i, (a, b) in enumerate(zip(clean, got)):
+            assert torch.equal(a[310 + 49 + 128:], b[310 + 49 + 128:]), (sinks, i)
+            first = 128 if sinks and i > 1 else 0  # (the first rows' keys are seen by the spoilt queries)
+            assert torch.equal(a[first:300 - 128], b[first:300 - 128]), (sinks, i)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_bands_of_one_buffer_and_rows_far_apart(gpu, dtype):
     """dq, dk and dv as bands of one buffer; tokens 2^24 bytes apart."""
     import torch
