@@ -514,8 +514,8 @@ typedef struct {
  * times the row's power of two where that is more. What is not finite is held
  * as NaN. Magnitudes of 248 * 2^120 and more are read back as infinity. */
 int proxy_paged_quant_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_quant_cache* cache,
-                        int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
-                        const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream);
+                             int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
+                             const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream);
 
 /* What rows of it stand for, in the config's dtype (exact in both): those rows
  * that an append of the same n_tokens and cu_tokens writes, into k_out and
@@ -523,16 +523,16 @@ int proxy_paged_quant_append(const pf_heads_config* cfg, const pf_heads_weights*
  * With cu_tokens the running sums of kv_len these are the whole sequences.
  * k_out and v_out overlap nothing else of the call. */
 int proxy_paged_quant_read(const pf_heads_config* cfg, const pf_paged_quant_cache* cache, int64_t n_tokens,
-                      const int32_t* cu_tokens, const pf_rows* k_out, const pf_rows* v_out, void* stream);
+                           const int32_t* cu_tokens, const pf_rows* k_out, const pf_rows* v_out, void* stream);
 
 /* Attention of new tokens over it, as proxy_paged_attention over what its rows
  * stand for (workspace: proxy_paged_quant_workspace_size bytes). */
 size_t proxy_paged_quant_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int32_t ragged,
-                                   int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks);
+                                        int64_t max_new, int64_t max_kv_len, int64_t window, int64_t sinks);
 int proxy_paged_quant_attention(const pf_heads_config* cfg, const pf_paged_quant_cache* cache, int64_t n_tokens,
-                           const int32_t* cu_tokens, const pf_rows* q, int64_t max_new, int64_t max_kv_len,
-                           int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace,
-                           size_t ws_bytes, void* stream);
+                                const int32_t* cu_tokens, const pf_rows* q, int64_t max_new, int64_t max_kv_len,
+                                int64_t window, int64_t sinks, float scale, void* out, float* lse, void* workspace,
+                                size_t ws_bytes, void* stream);
 
 /* Causal attention over whole sequences that lie one after another, in
  * training (or for prompts whose cache is written aside).
@@ -566,17 +566,18 @@ int proxy_packed_attention_forward(const pf_heads_config* cfg, int32_t batch, in
  * rounded once; in bf16 the weights and the scores' gradients are rounded to
  * bf16 in their products. What is not finite reaches other tokens as in the
  * forward, and from a token's dout and q the gradients of earlier rows whose
- * tiles it is in. Tokens behind the last sequence are left as they were. dq, dk and dv overlap neither each other nor what the call reads; they
- * may be bands of one buffer. workspace: proxy_packed_workspace_size bytes
- * (0 for invalid sizes), 16-byte aligned, overlapping nothing else; calls that
- * may run at the same time need workspaces of their own. */
+ * tiles it is in. Tokens behind the last sequence are left as they were.
+ * dq, dk and dv overlap neither each other nor what the call reads; they may
+ * be bands of one buffer. workspace: proxy_packed_workspace_size bytes (0 for
+ * invalid sizes), 16-byte aligned, overlapping nothing else; calls that may run
+ * at the same time need workspaces of their own. */
 size_t proxy_packed_workspace_size(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens, int64_t max_len,
                                    int64_t window, int64_t sinks);
 int proxy_packed_attention_backward(const pf_heads_config* cfg, int32_t batch, int64_t n_tokens,
                                     const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k, const pf_rows* v,
                                     int64_t max_len, int64_t window, int64_t sinks, float scale, const void* out,
-                                    const float* lse, const pf_rows* dout, const pf_rows* dq, const pf_rows* dk, const pf_rows* dv,
-                                    void* workspace, size_t ws_bytes, void* stream);
+                                    const float* lse, const pf_rows* dout, const pf_rows* dq, const pf_rows* dk,
+                                    const pf_rows* dv, void* workspace, size_t ws_bytes, void* stream);
 
 /* Launch tracing (profiling aid). While enabled, every kernel launch of the
  * library is bracketed by two HIP events recorded on its stream and

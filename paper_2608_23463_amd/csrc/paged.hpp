@@ -83,6 +83,32 @@ inline int64_t col_blocks(int cols, int group, int64_t n_tokens, int batch) {
   return n_tokens < 0 ? (int64_t)batch * ((group + cols - 1) / cols) : n_tokens * group / cols + batch;
 }
 
+// The head and the item of this workgroup among `per_head` of each of `hk`
+// K/V heads, a launch of their product. Workgroups go to the XCDs in turn; a
+// head's items stay on as few XCDs as its share of them (their L2s hold its
+// rows), and every XCD gets every rank of them, heavy ones first. Runs of a
+// CU's number of workgroups go up and down the ranks in turn, so where all are
+// resident at once a heavy one shares a CU with a light one.
+struct Item {
+  int hk, at;
+  __device__ __forceinline__ Item(int hks, const FastDiv& fhk, int per_head) {
+    constexpr int kCus = 32;  // of an XCD
+    const int id = (int)blockIdx.x;
+    int i;
+    if (hks % kNumXcd == 0) {
+      const int local = id / kNumXcd;
+      const int round = local / per_head;
+      hk = round * kNumXcd + id % kNumXcd;
+      i = local - round * per_head;
+    } else {
+      i = fhk.div(id);
+      hk = id - i * hks;
+    }
+    const int row = i / kCus, n = min(per_head - row * kCus, kCus);
+    at = row & 1 ? row * kCus + n - 1 - (i - row * kCus) : i;
+  }
+};
+
 // f over the wave, of values that are not negative, in every lane.
 template <class F>
 __device__ __forceinline__ int over_wave(int v, F&& f) {

@@ -46,17 +46,10 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
   constexpr int kPerTile = kTile / kBlock, kAhead = kWave / kPerTile;
   __shared__ __attribute__((aligned(1024))) char smem[2 * kStage];
 
-  // Every XCD takes a contiguous run of (K/V head, block), so the blocks of a
-  // head share an L2; within a head the blocks that see most rows come first.
+  // the blocks that see most rows come first
   const int total = (int)gridDim.x, blocks = p.fslices.div(total) / p.hk;
-  int at;
-  {
-    const int q = total / kNumXcd, rem = total % kNumXcd;
-    const int xcd = (int)blockIdx.x % kNumXcd, local = (int)blockIdx.x / kNumXcd;
-    at = (xcd < rem ? xcd * (q + 1) : rem * (q + 1) + (xcd - rem) * q) + local;
-  }
-  const int unit = p.fslices.div(at), slice = at - unit * p.slices;
-  const int hk = unit / blocks, rank = unit - hk * blocks;
+  const Item item(p.hk, p.fhk, blocks * p.slices);
+  const int hk = item.hk, rank = p.fslices.div(item.at), slice = item.at - rank * p.slices;
   Sequence sq;
   int s, x0;
   if (ranked(p, total)) {
