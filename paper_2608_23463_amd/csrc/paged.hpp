@@ -83,29 +83,30 @@ inline int64_t col_blocks(int cols, int group, int64_t n_tokens, int batch) {
   return n_tokens < 0 ? (int64_t)batch * ((group + cols - 1) / cols) : n_tokens * group / cols + batch;
 }
 
-// The head and the item of this workgroup among `per_head` of each of `hk`
+// The head and the item of this workgroup among `per_head` of each of `hks`
 // K/V heads, a launch of their product. Workgroups go to the XCDs in turn; a
 // head's items stay on as few XCDs as its share of them (their L2s hold its
-// rows), and every XCD gets every rank of them, heavy ones first. Runs of a
-// CU's number of workgroups go up and down the ranks in turn, so where all are
-// resident at once a heavy one shares a CU with a light one.
+// rows), and every XCD gets every rank of them, heavy ones first. Rounds of a
+// workgroup per CU go up and down the ranks in turn, so where all are resident
+// at once a heavy one shares a CU with a light one.
 struct Item {
   int hk, at;
   __device__ __forceinline__ Item(int hks, const FastDiv& fhk, int per_head) {
     constexpr int kCus = 32;  // of an XCD
     const int id = (int)blockIdx.x;
-    int i;
-    if (hks % kNumXcd == 0) {
-      const int local = id / kNumXcd;
-      const int round = local / per_head;
-      hk = round * kNumXcd + id % kNumXcd;
-      i = local - round * per_head;
-    } else {
+    int i, round;  // items of a head in a round
+    if (hks % kNumXcd == 0) {  // an XCD takes its heads one after another
+      const int local = id / kNumXcd, turn = local / per_head;
+      hk = turn * kNumXcd + id % kNumXcd;
+      i = local - turn * per_head;
+      round = kCus;
+    } else {  // all heads at once
       i = fhk.div(id);
       hk = id - i * hks;
+      round = max(kCus * kNumXcd / hks, 1);
     }
-    const int row = i / kCus, n = min(per_head - row * kCus, kCus);
-    at = row & 1 ? row * kCus + n - 1 - (i - row * kCus) : i;
+    const int row = i / round, n = min(per_head - row * round, round);
+    at = row & 1 ? row * round + n - 1 - (i - row * round) : i;
   }
 };
 
