@@ -287,6 +287,56 @@ def test_many_sequences(gpu, dtype):
             assert torch.equal(x, y[a:b])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_past_32_bits(gpu, dtype):
+    """The inputs' and gradients' rows 2^24 bytes apart, more than 4 GiB each
+    (out and lse are dense)."""
+    import torch
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    d, lens = 64, (130, 0, 150)
+    t = sum(lens)
+    cfg = gpu.heads_config(2, 1, d, dtype=dtype, norm=False, rot_dim=0)
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device="cuda")
+    step = (1 << 24) // dt.itemsize
+
+    def far(h):
+        return torch.empty((t - 1) * step + h * d, dtype=dt, device="cuda").as_strided((t, h, d), (step, d, 1))
+
+    near = {n: torch.randn(t, h, d, device="cuda").to(dt) for n, h in (("q", 2), ("k", 1), ("v", 1), ("do", 2))}
+    apart = {n: far(x.shape[1]).copy_(x) for n, x in near.items()}
+    out, lse = gpu.packed_attention_forward(cfg, near["q"], near["k"], near["v"], cu, 150)
+    want = out, lse, *gpu.packed_attention_backward(cfg, near["q"], near["k"], near["v"], out, lse, near["do"], cu, 150)
+    o, l = gpu.packed_attention_forward(cfg, apart["q"], apart["k"], apart["v"], cu, 150)
+    got = o, l, *gpu.packed_attention_backward(cfg, apart["q"], apart["k"], apart["v"], o, l, apart["do"], cu, 150, dq=far(2),
+                                               dk=far(1), dv=far(1))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_tokens_past_32_bits(gpu):
+    """90,000 sequences whose tensors hold more than 4 GiB each: those around
+    2 and 4 GiB and the last against themselves alone."""
+    import torch
+    lens = np.random.default_rng(13).integers(0, 201, 90000)
+    ends = np.concatenate([[0], np.cumsum(lens)])
+    cu = torch.from_numpy(ends.astype(np.int32)).cuda()
+    t, d = int(ends[-1]), 64
+    assert t * 4 * d * 2 > 1 << 32
+    cfg = gpu.heads_config(4, 4, d, norm=False, rot_dim=0)
+    q, k, v, do = (torch.randn(t, 4, d, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+    out, lse = gpu.packed_attention_forward(cfg, q, k, v, cu, 200)
+    got = gpu.packed_attention_backward(cfg, q, k, v, out, lse, do, cu, 200)
+    seqs = [int(np.searchsorted(ends, n // (4 * d * 2), "right")) - 1 + i for n in (1 << 31, 1 << 32) for i in range(-2, 3)]
+    for s in seqs + [0, 89997, 89998, 89999]:
+        a, b = int(ends[s]), int(ends[s + 1])
+        if a == b:
+            continue
+        one = torch.tensor([0, b - a], dtype=torch.int32, device="cuda")
+        o, l = gpu.packed_attention_forward(cfg, q[a:b], k[a:b], v[a:b], one, 200)
+        alone = gpu.packed_attention_backward(cfg, q[a:b], k[a:b], v[a:b], o, l, do[a:b], one, 200)
+        for x, y in zip((o, l, *alone), (out, lse, *got)):
+            assert torch.equal(x, y[a:b]), s
+
+
 def test_max_len_lays_out_only(gpu):
     """A launch laid out for fewer or more tokens than there are is right too."""
     import torch
