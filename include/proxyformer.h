@@ -5,7 +5,8 @@
  * block compression, causal multi-head attention over the L/P proxies,
  * decompression and gated injection back into every token), its backward,
  * and the proxy-only KV-cache decode step with its block-triggered append
- * (Sec. 3.8, Eq. 19-21). Every step runs in hand-written HIP kernels.
+ * (Sec. 3.8, Eq. 19-21); and the fine tokens' own attention: over a paged cache
+ * of 16, 32 or 8 bits, and over whole packed sequences, with its backward. Every step runs in hand-written HIP kernels.
  *
  * Conventions shared by every entry point
  *  - Tensor arguments are DEVICE pointers owned by the caller: contiguous,

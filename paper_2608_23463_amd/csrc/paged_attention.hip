@@ -25,6 +25,11 @@
 //    Lane (m, g) loads VE neighbouring channels VE m .. of the same rows, and
 //    the e-th instruction takes channel e of every lane: its m index stands for
 //    channel VE m + e. In bf16 one permute joins two rows of a channel.
+//
+// Pages of 8 bits: the codes become the values of a wider cache (a power of two
+// times e4m3 is exact in bf16 and in fp32) where an instruction takes them; the
+// rest is the same. 32 sequences of 16,384 rows, 16 heads of 64, 209 us, 368 over
+// bf16 pages.
 #include <algorithm>
 
 #include "paged.hpp"

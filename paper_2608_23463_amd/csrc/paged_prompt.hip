@@ -1,5 +1,9 @@
-// Attention of prompts over a paged cache, bf16 (the mathematics and the
-// columns are those of paged_attention.hip; here a workgroup has 128 of them).
+// Attention of prompts in bf16 (the mathematics and the columns are those of
+// paged_attention.hip; here a workgroup has 128 of them). Its rows come from
+// bf16 pages, from pages of 8 bits, or from the tokens' own rows (whole sequences
+// in training). 8 bits take 20 to 25 per cent longer (five prompts of up to 1,800
+// tokens behind up to 6,000 rows, 32 over 8 heads of 128, 389 us, 321 from bf16
+// pages): their rows pass through registers and LDS stores.
 //
 // Bound by the matrix cores and the exponentials: 4 D flops per (column, row)
 // that is seen. 128 columns per workgroup, 32 per wave; tiles of 64 rows of K
@@ -12,7 +16,7 @@
 // leaves its registers. Q is not scaled beforehand (its bf16 would round):
 // the scale is part of the one multiply-add in front of each exponential. Waves
 // in their matrix phases go before those in their exponentials (8,192 tokens, 32
-// over 8 heads of 128, 523 us, without it 545).
+// over 8 heads of 128, 531 us, without it 551; packed 558 and 592).
 //
 // The weights are rounded to bf16 once: 2^-8 of each at most, independent of
 // one another. With many rows that is as much as the rounding of the result, so
@@ -33,10 +37,10 @@ constexpr int kThreads = 256;
 constexpr int kTile = 64;
 constexpr int kColumns = 128;
 
-// Three workgroups per CU at 64 channels (16 heads: six windowed prompts 44 us,
-// with two 56, four of 4,096 tokens behind 16,384 rows 1,347 and 1,516; one of
-// 8,192 tokens, a round and a half of workgroups, 195 and 173), two at 128, whose
-// accumulators take the registers of a third.
+// Three workgroups per CU at 64 channels (16 heads: six windowed prompts 41 us,
+// with two 53, four of 4,096 tokens behind 16,384 rows 1,382 and 1,462; one of
+// 8,192 tokens 179 and 196; 20 windowed sequences in training 113 and 134), two at
+// 128, whose accumulators take the registers of a third.
 template <int D, Source FROM>
 __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel(PagedParams p) {
   constexpr int RB = D * 2, CH = RB / 16;     // bytes and 16-byte chunks of a row
