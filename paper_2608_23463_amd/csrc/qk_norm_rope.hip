@@ -259,11 +259,12 @@ __device__ __forceinline__ void load_gain(const QkParams& p, const Tensor& x, in
 // into pages of the rows' type or of 8 bits.
 enum Mode { kTurn, kAppend, kAppend8 };
 
-// Norm and rotation of the lane's 16 elements of a row. FINE: in 64 bits, for
-// keys that are held in 8, whose values next to a border each error on the way
-// moves by a whole step. Element after element: side by side the products would
-// cost the registers of a workgroup (24 prompts of up to 2,600 tokens, 32 over 8
-// heads of 128, 190 us for 163, 152 in 32 bits).
+// Norm and rotation of the lane's 16 elements of a row. FINE: for keys that are
+// held in 8 bits, whose values next to a border each error on the way moves by a
+// whole step: the norm in 64 bits, rounded to fp32, then the turn in 64 bits by a
+// cosine and a sine in fp32, rounded to it again. Element after element: side by
+// side the products would cost the registers of a workgroup (24 prompts of up to
+// 2,600 tokens, 32 over 8 heads of 128, 190 us for 163, 152 in 32 bits).
 template <int D, bool PAIRS, bool FINE>
 __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, float* v, const float* g, const float2* cs,
                                               bool turned) {
@@ -276,9 +277,8 @@ __device__ __forceinline__ void norm_and_turn(const QkParams& p, int which, floa
         ss += (double)v[i] * v[i];
         asm volatile("" : "+v"(ss));
       }
-      const double m = row_sum<D / 16>(ss) * (1.0 / D) + p.eps;
-      double r = rsqrtf((float)m);
-      r *= 1.5 - 0.5 * m * r * r;  // of 2^-23 of the root 2^-45
+      // (the mean of squares may be past fp32's range where the row is not)
+      const double r = rsqrt(row_sum<D / 16>(ss) * (1.0 / D) + p.eps);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         float gain = g[i];
