@@ -6,7 +6,8 @@
  * decompression and gated injection back into every token), its backward,
  * and the proxy-only KV-cache decode step with its block-triggered append
  * (Sec. 3.8, Eq. 19-21); and the fine tokens' own attention: over a paged cache
- * of 16, 32 or 8 bits, and over whole packed sequences, with its backward. Every step runs in hand-written HIP kernels.
+ * of 16, 32 or 8 bits, and over whole packed sequences, with its backward. Every
+ * step runs in hand-written HIP kernels.
  *
  * Conventions shared by every entry point
  *  - Tensor arguments are DEVICE pointers owned by the caller: contiguous,
@@ -358,7 +359,9 @@ int proxy_decode_prefill(const pf_decode_config* cfg, const pf_decode_weights* w
  *   y_a = z_a cos t - z_b sin t, y_b = z_a sin t + z_b cos t.
  * The angle is formed in 64 bits and keeps to 2^-51 of itself: 1e-6 at 2^31
  * radians.
- * Sums and statistics are fp32; a row is rounded once, when it is stored. */
+ * Sums and statistics are fp32; a row is rounded once, when it is stored (keys
+ * into a cache of 8 bits apart). A row whose mean square passes fp32's range
+ * comes out as zeros. */
 #define PF_MAX_AXES 3
 enum pf_head_norm { PF_NORM_NONE = 0, PF_NORM_RMS = 1 };
 enum pf_rope_style { PF_ROPE_HALVES = 0, PF_ROPE_PAIRS = 1 };
@@ -501,25 +504,31 @@ int proxy_paged_attention(const pf_heads_config* cfg, const pf_paged_cache* cach
  * (the OCP 8-bit format with four exponent bits), one byte per element, and
  * k_scales, v_scales [n_pages, n_kv_heads, page_size] a byte s for every row of
  * a head: an element stands for code * 2^(s - 127). Everything else is as in
- * pf_paged_cache; the bytes that rows are read with lie in 1..254. */
+ * pf_paged_cache; the bytes that rows are read with lie in 1..254. Bytes of
+ * 3..246 stand for values that bf16 and fp32 hold exactly. Values under 1 and 2
+ * are rounded in bf16, to multiples of 2^-133; those of 2^128 and more, under
+ * 247..254, are infinities in both. */
 typedef struct {
   pf_paged_cache pages;
   uint8_t* k_scales;
   uint8_t* v_scales;
 } pf_paged_quant_cache;
 
-/* New tokens into it, as proxy_paged_append. A row x, normed and turned in
- * fp32, is held with the smallest s of 17..247 with max |x| <= 448 * 2^(s - 127),
- * the largest over its finite elements, and each element as x * 2^(127 - s)
- * rounded to e4m3, to nearest even: off by at most 2^-4 of itself, or 2^-10
- * times the row's power of two where that is more. What is not finite is held
- * as NaN. Magnitudes of 248 * 2^120 and more are read back as infinity. */
+/* New tokens into it, as proxy_paged_append. Keys are normed in 64 bits and
+ * rounded to fp32, then turned in 64 bits by cosines and sines in fp32 and
+ * rounded to fp32 again (their mean squares may pass fp32's range). A row x, a
+ * key's after that, is held with the smallest s of 17..247 with
+ * max |x| <= 448 * 2^(s - 127), the largest over its finite elements, and each
+ * element as x * 2^(127 - s) rounded to e4m3, to nearest even: off by at most
+ * 2^-4 of itself, or 2^-10 times the row's power of two where that is more. What
+ * is not finite is held as NaN. Magnitudes of 248 * 2^120 and more are read back
+ * as infinity. */
 int proxy_paged_quant_append(const pf_heads_config* cfg, const pf_heads_weights* w, const pf_paged_quant_cache* cache,
                              int64_t n_tokens, const int32_t* cu_tokens, const pf_rows* q, const pf_rows* k,
                              const pf_rows* v, const int32_t* positions, const pf_rows* q_out, void* stream);
 
-/* What rows of it stand for, in the config's dtype (exact in both): those rows
- * that an append of the same n_tokens and cu_tokens writes, into k_out and
+/* What rows of it stand for, in the config's dtype (as exact as said above):
+ * those rows that an append of the same n_tokens and cu_tokens writes, into k_out and
  * v_out [n_tokens, n_kv_heads] rows. Tokens without a place are left alone.
  * With cu_tokens the running sums of kv_len these are the whole sequences.
  * k_out and v_out overlap nothing else of the call. */
@@ -553,7 +562,8 @@ int proxy_paged_quant_attention(const pf_heads_config* cfg, const pf_paged_quant
  * does not see has no weight in its result; of the rows that other tokens of
  * its tile see it is taken times zero, so an infinity or a NaN in one of those
  * can reach it. Other sequences' rows cannot. In bf16 the weights are rounded
- * to bf16 in their product with the values (their sum before that).
+ * to bf16 in their product with the values (their sum before that). Values of a
+ * magnitude below 2^80 give finite results, whatever the finite scores.
  * n_tokens * n_heads below 2^31, n_tokens * n_heads / 128 + batch * n_kv_heads
  * below 2^24; n_tokens = 0 does nothing. out and lse overlap nothing else of
  * the call. The result is the same in every run. */
