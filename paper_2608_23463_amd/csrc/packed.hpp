@@ -10,8 +10,8 @@ namespace pf {
 // A call's parameters as the kernels take them.
 PagedParams packed_params(const HeadsDims& d, const PackedCall& c);
 
-// The gradients' part of a call. PagedParams holds the rest (no pages: kv_len
-// is NULL, a sequence's tokens are its rows).
+// The gradients' part of a call. PagedParams holds the rest (no pages: a
+// sequence's tokens are its rows).
 struct PackedGrads {
   const char* dout;
   int64_t do_ts, do_hs;
@@ -163,13 +163,13 @@ struct Columns {
     hk = item.hk;
     // the columns that see most come first
     if (ranked(p, (int)gridDim.x)) {
-      const Ranked r(item.at, p.batch, kPackedCols, p);
+      const Ranked<true> r(item.at, p.batch, kPackedCols, p);
       any = r.seq >= 0;
-      sq.set(p, any ? r.seq : 0);
+      sq.set<true>(p, any ? r.seq : 0);
       x0 = any ? r.block * kPackedCols : 0;
     } else {
       const int blk = blocks - 1 - item.at, s = sequence_of_block<kPackedCols>(p, blk);
-      sq.set(p, s);
+      sq.set<true>(p, s);
       x0 = (blk - first_block<kPackedCols>(p, s)) * kPackedCols;
       any = sq.seq >= 0 && x0 >= 0 && x0 < sq.cols;
     }

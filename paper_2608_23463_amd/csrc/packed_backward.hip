@@ -58,7 +58,7 @@ struct KeyBlock {
   __device__ __forceinline__ KeyBlock(const PagedParams& p, const PackedGrads& z, int hk_, int blk_, int slice)
       : hk(hk_), blk(blk_) {
     s = find_run(p.batch, [&](int c) { return p.cu[c] / kKeys + c; }, blk);
-    sq.set(p, s);
+    sq.set<true>(p, s);
     n = sq.seq < 0 ? 0 : p.fgroup.div(sq.cols);
     k0 = (blk - (p.cu[s] / kKeys + s)) * kKeys;
     any = k0 >= 0 && k0 < n;

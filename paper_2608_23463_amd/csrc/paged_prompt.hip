@@ -57,15 +57,15 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) paged_prompt_kernel
   Sequence sq;
   int s, x0;
   if (ranked(p, total)) {
-    const Ranked r(rank, p.batch, kColumns, p);
+    const Ranked<FROM == kPacked> r(rank, p.batch, kColumns, p);
     if (r.seq < 0) return;
     s = r.seq;
-    sq.set(p, s);
+    sq.set<FROM == kPacked>(p, s);
     x0 = r.block * kColumns;
   } else {
     const int blk = blocks - 1 - rank;
     s = sequence_of_block<kColumns>(p, blk);
-    sq.set(p, s);
+    sq.set<FROM == kPacked>(p, s);
     x0 = (blk - first_block<kColumns>(p, s)) * kColumns;
     if (sq.seq < 0 || x0 < 0 || x0 >= sq.cols) return;
   }
