@@ -1,6 +1,6 @@
 // Rows of an 8-bit cache back into the rows' type: codes times their row's power
 // of two, exact in bf16 and in fp32. Bound by HBM: 1 + es bytes per element
-// (24 sequences of up to 7,000 rows, 8 heads of 128, 134 us, 4.8 TB/s; with 32 bytes of a
+// (24 sequences of up to 7,000 rows, 8 heads of 128, 131 us, 4.9 TB/s; with 32 bytes of a
 // lane's written side by side 160).
 #include "paged.hpp"
 #include "trace.hpp"
@@ -12,6 +12,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kMostTokens = 4;  // of a wave
+
+// A wave takes one token where its rows of K and V fill more than half of the four
+// passes that load together, or where waves are few; else kMostTokens. 168,000 tokens
+// of 2 x 64 in bf16 30 us (a token each 77), 4 x 128 104 (134), 12 x 64 168 (165), 16 x
+// 64 223 (208), 8 x 128 in fp32 355 (337); 8,192 of 8 x 64 8.7 us (9.2), 4,096 of them 7.4
+// (6.6), 150 6.2 (4.9).
+constexpr int kManyTokens = 8192, kFewBytes = 1024;  // bytes of a token's K in the rows' type
 
 struct Read8Params {
   const char* k;
@@ -129,7 +136,7 @@ hipError_t launch_paged_quant_read(const HeadsDims& d, const PagedDims& c, int64
   p.fpage = FastDiv(c.page_size);
   p.fhk = FastDiv(d.hk);
   p.n = n;
-  p.tokens = n >= 65536 ? 4 : 1;
+  p.tokens = n >= kManyTokens && d.hk * d.d * d.esize <= kFewBytes ? kMostTokens : 1;
   p.k_out = k_out;
   p.v_out = v_out;
   return timed("paged_quant_read", s, [&] { d.esize == 2 ? read_on<bf16>(d, p, s) : read_on<float>(d, p, s); });

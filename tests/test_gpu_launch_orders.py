@@ -191,11 +191,11 @@ def test_prompts(gpu, name, bits8):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("hk, d", [(2, 64), (1, 128)])
+@pytest.mark.parametrize("hk, d", [(2, 64), (1, 128), (16, 64), (8, 128)])
 def test_a_large_read(gpu, dtype, hk, d):
-    """More than 65,536 tokens (from there on a wave takes four): long sequences
-    between thousands of none to five rows, rows before 0, entries that are no page,
-    tokens behind the last sequence; the values bit for bit."""
+    """More than 65,536 tokens of few heads (a wave takes four of them) and many (one):
+    long sequences between thousands of none to five rows, rows before 0, entries that
+    are no page, tokens behind the last sequence; the values bit for bit."""
     import torch
     gen = torch.Generator(device="cuda").manual_seed(4)
     rng = np.random.default_rng(4)
