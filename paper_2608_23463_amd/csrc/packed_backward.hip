@@ -256,7 +256,13 @@ __global__ void __launch_bounds__(kThreads) packed_join_kernel(PagedParams p, Pa
 // In bf16 D_i comes from the rounded O, an error as large as the others in the
 // scores' gradients where a query sees few keys. But these add up to zero over
 // a query's keys, so what they add up to corrects D: for the kernel of dK and dV,
-// which runs behind this one, and where a workgroup sees few tiles for dQ too.
+// which runs behind this one, and where a workgroup sees few tiles for dQ too, by a
+// pass beforehand. dQ's error over that of the rounded exact result, and the time of
+// the whole backward (8,192 tokens, 32 over 8 heads of 128), with that pass over up to
+// 4 tiles, 2 and none: documents of 64 tokens 1.415 and 138 us, the same, 1.60 and 134;
+// of 320 1.424 and 190 us, 1.427 and 182, 1.54 and 179; of 512 1.423 and 266 us, 1.426
+// and 240, 1.52 and 240; windows of 200 1.426 and 208 us, 1.433 and 187, 1.46 and 189.
+// Over up to 5 and 8 the errors are those of 4, 1.41 being the two roundings' own.
 constexpr int kFewTiles = 4;
 
 template <typename T, int D>

@@ -214,7 +214,7 @@ __device__ __forceinline__ float scale_in(uint32_t word, int row) {
 }
 
 // Two neighbouring e4m3 values, the lower or the upper half of a word, times a
-// power of two: exact in bf16 and in fp32.
+// power of two: exact in bf16 and in fp32 (scale bytes of 3 to 246).
 template <bool UPPER>
 __device__ __forceinline__ uint32_t bf16_pair_of(uint32_t w, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, UPPER));

@@ -1,5 +1,5 @@
 // Rows of an 8-bit cache back into the rows' type: codes times their row's power
-// of two, exact in bf16 and in fp32. Bound by HBM: 1 + es bytes per element
+// of two, exact in bf16 and in fp32 (scale bytes of 3 to 246). Bound by HBM: 1 + es bytes per element
 // (24 sequences of up to 7,000 rows, 8 heads of 128, 131 us, 4.9 TB/s; with 32 bytes of a
 // lane's written side by side 160).
 #include "paged.hpp"
